@@ -18,6 +18,8 @@ FP32 = 0
 BF16 = 1
 HEAD_RNN = 0
 HEAD_MARKOV = 1
+CACHE_BF16 = 0
+CACHE_E4M3 = 1
 
 OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_WORKSPACE, ERR_HIP, ERR_ORDER, ERR_NONFINITE = range(7)
 
@@ -44,6 +46,13 @@ SYMBOLS = [
     "dartree_accept_walk", "dartree_tree_attention_workspace_size", "dartree_tree_attention",
     "dartree_calib_read", "dartree_calib_copy", "dartree_calib_mfma", "dartree_calib_empty",
     "dartree_calib_grid_barrier",
+]
+# include/dartree/serve.h
+SERVE_SYMBOLS = [
+    "dartree_cache_validate", "dartree_cache_write", "dartree_cache_read",
+    "dartree_tree_attention_paged_workspace_size", "dartree_tree_attention_paged",
+    "dartree_verify_tree_workspace_size", "dartree_verify_tree",
+    "dartree_verify_chain_workspace_size", "dartree_verify_chain",
 ]
 CALIB_MAX_BARRIERS = 64
 CALIB_SINK_FLOATS = 4096
@@ -98,6 +107,17 @@ class AttnParams(ctypes.Structure):
     _fields_ = [("batch", ctypes.c_int32), ("budget", ctypes.c_int32), ("max_ctx", ctypes.c_int32),
                 ("heads_q", ctypes.c_int32), ("heads_kv", ctypes.c_int32), ("head_dim", ctypes.c_int32),
                 ("scale", ctypes.c_float)]
+
+
+class CacheParams(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("heads_kv", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("page", ctypes.c_int32), ("num_pages", ctypes.c_int32), ("max_pages", ctypes.c_int32),
+                ("type", ctypes.c_int32)]
+
+
+class CacheC(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_exp", ctypes.c_void_p),
+                ("v_exp", ctypes.c_void_p), ("table", ctypes.c_void_p)]
 
 
 class DartreeError(RuntimeError):
@@ -155,7 +175,18 @@ def lib() -> ctypes.CDLL:
     L.dartree_calib_mfma.argtypes = [i32, i32, vp, vp]
     L.dartree_calib_empty.argtypes = [i32, vp]
     L.dartree_calib_grid_barrier.argtypes = [i32, i32, vp, vp, vp]
-    for name in SYMBOLS:
+    C, A = ctypes.POINTER(CacheParams), ctypes.POINTER(AttnParams)
+    L.dartree_cache_validate.argtypes = [C]
+    L.dartree_cache_write.argtypes = [C, ctypes.POINTER(CacheC), i32, i32, vp, vp, i64, vp, vp, vp, vp]
+    L.dartree_cache_read.argtypes = [C, ctypes.POINTER(CacheC), i32, vp, vp, vp, vp, vp]
+    L.dartree_tree_attention_paged_workspace_size.argtypes = [A, C, ctypes.POINTER(sz)]
+    L.dartree_tree_attention_paged.argtypes = [A, C, ctypes.POINTER(CacheC), vp, i64, vp, vp, i64, vp, vp, vp, vp, vp,
+                                               sz, vp]
+    L.dartree_verify_tree_workspace_size.argtypes = [i32, i32, i32, i32, ctypes.POINTER(sz)]
+    L.dartree_verify_tree.argtypes = [i32, i32, i32, i32, i32, vp, vp, vp, vp, i64, f32, vp, vp, vp, vp, vp, sz, vp]
+    L.dartree_verify_chain_workspace_size.argtypes = [i32, i32, i32, ctypes.POINTER(sz)]
+    L.dartree_verify_chain.argtypes = [i32, i32, i32, i32, vp, vp, vp, vp, i64, f32, vp, vp, vp, vp, sz, vp]
+    for name in SYMBOLS + SERVE_SYMBOLS:
         if name not in ("dartree_abi_version", "dartree_status_string"):
             getattr(L, name).restype = ctypes.c_int
     _lib = L
@@ -534,3 +565,260 @@ def tree_attention(p: AttnParams, q, k_ctx, v_ctx, k_tree, v_tree, mask, ctx_len
     _check(lib().dartree_tree_attention(ctypes.byref(p), _ptr(q), _ptr(k_ctx), _ptr(v_ctx), _ptr(k_tree),
                                         _ptr(v_tree), _ptr(mask), _ptr(ctx_len), _ptr(out), _ptr(ws),
                                         0 if ws is None else ws.numel(), _stream(stream)), "dartree_tree_attention")
+
+
+# ---------------------------------------------------------------------------
+# Serving: a paged cache, attention over it, verification (dartree/serve.h)
+# ---------------------------------------------------------------------------
+def _want(where: str, **tensors) -> None:
+    """Each tensor (None: not given) on the current device and, unless its name
+    ends in _rows (checked by its caller), dense; ValueError otherwise."""
+    import torch
+    device = torch.cuda.current_device() if torch.cuda.is_available() else -1
+    for name, t in tensors.items():
+        if t is None:
+            continue
+        if t.get_device() != device:
+            raise ValueError(f"{where}: {name} is on {t.device}, not on the current device")
+        if not name.endswith("_rows") and not t.is_contiguous():
+            raise ValueError(f"{where}: {name} is not contiguous")
+
+
+def _row_stride(where: str, name: str, t) -> int:
+    """Elements between the rows of t [b][rows][heads][128]: heads are dense,
+    rows may be apart, requests follow each other."""
+    b, rows, heads, dim = t.shape
+    st = t.stride()
+    if st[3] != 1 or (heads > 1 and st[2] != dim) or (b > 1 and st[0] != rows * st[1]):
+        raise ValueError(f"{where}: {name} is neither dense nor rows of a wider tensor")
+    if rows > 1:
+        return st[1]
+    return st[0] if b > 1 else heads * dim
+
+
+def _bf16(where: str, **tensors) -> None:
+    for name, t in tensors.items():
+        if str(t.dtype) != "torch.bfloat16":
+            raise ValueError(f"{where}: {name} is {t.dtype}, not bfloat16")
+
+
+def _int32(where: str, **tensors) -> None:
+    for name, t in tensors.items():
+        if t is not None and str(t.dtype) != "torch.int32":
+            raise ValueError(f"{where}: {name} is {t.dtype}, not int32")
+
+
+def _shape(where: str, name: str, t, want: tuple) -> None:
+    if t is not None and tuple(t.shape) != want:
+        raise ValueError(f"{where}: {name} is {tuple(t.shape)}, not {want}")
+
+
+@dataclasses.dataclass
+class DeviceCache:
+    """Pages k, v [num_pages][heads_kv][page][128] (bfloat16 or float8_e4m3fn),
+    k_exp, v_exp uint8 [num_pages][heads_kv][page] (e4m3 only), table int32
+    [b][max_pages]."""
+    k: object
+    v: object
+    k_exp: object
+    v_exp: object
+    table: object
+
+    def c(self) -> CacheC:
+        return CacheC(_ptr(self.k), _ptr(self.v), _ptr(self.k_exp), _ptr(self.v_exp), _ptr(self.table))
+
+    @staticmethod
+    def alloc(p: CacheParams, device="cuda") -> "DeviceCache":
+        """Pages of undefined contents; every table entry -1 (no page)."""
+        import torch
+        eight = p.type == CACHE_E4M3
+        shape = (p.num_pages, p.heads_kv, p.page)
+        pages = lambda: (torch.empty(*shape, p.head_dim, dtype=torch.uint8, device=device).view(torch.float8_e4m3fn)
+                         if eight else torch.empty(*shape, p.head_dim, dtype=torch.bfloat16, device=device))
+        exps = lambda: torch.empty(shape, dtype=torch.uint8, device=device) if eight else None
+        return DeviceCache(pages(), pages(), exps(), exps(),
+                           torch.full((p.batch, p.max_pages), -1, dtype=torch.int32, device=device))
+
+    def check(self, p: CacheParams, where: str) -> None:
+        shape = (p.num_pages, p.heads_kv, p.page)
+        eight = p.type == CACHE_E4M3
+        for name in ("k", "v"):
+            t = getattr(self, name)
+            _shape(where, name, t, (*shape, p.head_dim))
+            if t.element_size() != (1 if eight else 2):
+                raise ValueError(f"{where}: cache {name} is {t.dtype}")
+            if eight:
+                e = getattr(self, name + "_exp")
+                _shape(where, name + "_exp", e, shape)
+                if e is not None and e.element_size() != 1:
+                    raise ValueError(f"{where}: cache {name}_exp is {e.dtype}")
+        _shape(where, "table", self.table, (p.batch, p.max_pages))
+        _int32(where, table=self.table)
+        _want(where, k=self.k, v=self.v, k_exp=self.k_exp, v_exp=self.v_exp, table=self.table)
+
+
+def cache_validate(p: CacheParams) -> int:
+    return lib().dartree_cache_validate(None if p is None else ctypes.byref(p))
+
+
+def cache_write(p: CacheParams, cache: DeviceCache, k, v, rows: int, index=None, counts=None, start=None,
+                stream=None) -> None:
+    """Position start[q] + i of request q, i < counts[q] <= rows, takes row
+    index[q][i] (None: i) of k and v [b][source_rows][heads_kv][128] bfloat16
+    (rows of a wider tensor are taken as they are)."""
+    where = "cache_write"
+    cache.check(p, where)
+    _want(where, k_rows=k, v_rows=v, index=index, counts=counts, start=start)
+    _bf16(where, k=k, v=v)
+    _int32(where, index=index, counts=counts, start=start)
+    src = k.shape[1]
+    for name, t in (("k", k), ("v", v)):
+        _shape(where, name, t, (p.batch, src, p.heads_kv, p.head_dim))
+    _shape(where, "index", index, (p.batch, rows))
+    _shape(where, "counts", counts, (p.batch,))
+    _shape(where, "start", start, (p.batch,))
+    stride = _row_stride(where, "k", k)
+    if _row_stride(where, "v", v) != stride:
+        raise ValueError(f"{where}: the rows of k and v are not equally far apart")
+    cc = cache.c()
+    _check(lib().dartree_cache_write(ctypes.byref(p), ctypes.byref(cc), src, rows, _ptr(k), _ptr(v), stride, _ptr(index),
+                                     _ptr(counts), _ptr(start), _stream(stream)), "dartree_cache_write")
+
+
+def cache_read(p: CacheParams, cache: DeviceCache, k, v, counts=None, start=None, stream=None) -> None:
+    """Rows i < counts[q] of k, v [b][rows][heads_kv][128] bfloat16 take the
+    cache's positions start[q] + i."""
+    where = "cache_read"
+    cache.check(p, where)
+    _want(where, k=k, v=v, counts=counts, start=start)
+    _bf16(where, k=k, v=v)
+    _int32(where, counts=counts, start=start)
+    rows = k.shape[1]
+    for name, t in (("k", k), ("v", v)):
+        _shape(where, name, t, (p.batch, rows, p.heads_kv, p.head_dim))
+    _shape(where, "counts", counts, (p.batch,))
+    _shape(where, "start", start, (p.batch,))
+    cc = cache.c()
+    _check(lib().dartree_cache_read(ctypes.byref(p), ctypes.byref(cc), rows, _ptr(k), _ptr(v), _ptr(counts), _ptr(start),
+                                    _stream(stream)), "dartree_cache_read")
+
+
+def tree_attention_paged_workspace_size(a: AttnParams, p: CacheParams) -> int:
+    n = ctypes.c_size_t(0)
+    _check(lib().dartree_tree_attention_paged_workspace_size(ctypes.byref(a), ctypes.byref(p), ctypes.byref(n)),
+           "dartree_tree_attention_paged_workspace_size")
+    return n.value
+
+
+def tree_attention_paged(a: AttnParams, p: CacheParams, cache: DeviceCache, q, k_tree, v_tree, mask, ctx_len, out, ws,
+                         num_nodes=None, stream=None) -> None:
+    """q [b][B][heads_q][128], k_tree, v_tree [b][B][heads_kv][128] bfloat16 (rows
+    of a wider tensor are taken as they are), mask int64 [b][B][ceil(B/64)]
+    (None: a chain), out bfloat16 [b][B][heads_q][128]."""
+    where = "tree_attention_paged"
+    cache.check(p, where)
+    _want(where, q_rows=q, k_rows=k_tree, v_rows=v_tree, mask=mask, ctx_len=ctx_len, num_nodes=num_nodes, out=out, ws=ws)
+    _bf16(where, q=q, k_tree=k_tree, v_tree=v_tree, out=out)
+    _int32(where, ctx_len=ctx_len, num_nodes=num_nodes)
+    b, n = a.batch, a.budget
+    for name, t, heads in (("q", q, a.heads_q), ("k_tree", k_tree, a.heads_kv), ("v_tree", v_tree, a.heads_kv),
+                           ("out", out, a.heads_q)):
+        _shape(where, name, t, (b, n, heads, a.head_dim))
+    _want(where, out=out)
+    if mask is not None:
+        _shape(where, "mask", mask, (b, n, (n + 63) // 64))
+        if mask.element_size() != 8:
+            raise ValueError(f"{where}: mask is {mask.dtype}")
+    _shape(where, "ctx_len", ctx_len, (b,))
+    _shape(where, "num_nodes", num_nodes, (b,))
+    stride = _row_stride(where, "k_tree", k_tree)
+    if _row_stride(where, "v_tree", v_tree) != stride:
+        raise ValueError(f"{where}: the rows of k_tree and v_tree are not equally far apart")
+    cc = cache.c()
+    _check(lib().dartree_tree_attention_paged(ctypes.byref(a), ctypes.byref(p), ctypes.byref(cc), _ptr(q),
+                                              _row_stride(where, "q", q), _ptr(k_tree), _ptr(v_tree), stride, _ptr(mask),
+                                              _ptr(num_nodes), _ptr(ctx_len), _ptr(out), _ptr(ws),
+                                              0 if ws is None else ws.numel() * ws.element_size(), _stream(stream)),
+           "dartree_tree_attention_paged")
+
+
+def _logits(where: str, name: str, t, shape: tuple) -> tuple:
+    """(logits type, elements between rows) of [b][rows][vocab] logits whose rows may be apart."""
+    kind = {"torch.float32": FP32, "torch.bfloat16": BF16}.get(str(t.dtype))
+    if kind is None:
+        raise ValueError(f"{where}: {name} is {t.dtype}")
+    _shape(where, name, t, shape)
+    b, rows, vocab = shape
+    st = t.stride()
+    if (vocab > 1 and st[2] != 1) or (b > 1 and rows > 1 and st[0] != rows * st[1]):
+        raise ValueError(f"{where}: {name} is neither dense nor rows of a wider tensor")
+    return kind, st[1] if rows > 1 else st[0] if b > 1 else vocab
+
+
+def verify_tree_workspace_size(batch: int, budget: int, max_len: int, vocab: int) -> int:
+    n = ctypes.c_size_t(0)
+    _check(lib().dartree_verify_tree_workspace_size(batch, budget, max_len, vocab, ctypes.byref(n)),
+           "dartree_verify_tree_workspace_size")
+    return n.value
+
+
+def verify_chain_workspace_size(batch: int, depth: int, vocab: int) -> int:
+    n = ctypes.c_size_t(0)
+    _check(lib().dartree_verify_chain_workspace_size(batch, depth, vocab, ctypes.byref(n)),
+           "dartree_verify_chain_workspace_size")
+    return n.value
+
+
+def verify_tree(tokens, parents, num_nodes, target_logits, temperature: float, uniforms, accepted, num_accepted, bonus, ws,
+                stream=None) -> None:
+    """tokens, parents [b][B] and num_nodes [b] of emitted trees, target_logits
+    [b][B+1][V] float32 or bfloat16, uniforms float32 [b][B+1]; outputs accepted
+    [b][max_len], num_accepted [b], bonus [b] (int32)."""
+    where = "verify_tree"
+    b, n = tokens.shape
+    vocab, max_len = target_logits.shape[-1], accepted.shape[1]
+    _want(where, tokens=tokens, parents=parents, num_nodes=num_nodes, logits_rows=target_logits, uniforms=uniforms,
+          accepted=accepted, num_accepted=num_accepted, bonus=bonus, ws=ws)
+    _int32(where, tokens=tokens, parents=parents, num_nodes=num_nodes, accepted=accepted, num_accepted=num_accepted,
+           bonus=bonus)
+    kind, stride = _logits(where, "target_logits", target_logits, (b, n + 1, vocab))
+    _shape(where, "parents", parents, (b, n))
+    _shape(where, "uniforms", uniforms, (b, n + 1))
+    _shape(where, "accepted", accepted, (b, max_len))
+    for name, t in (("num_nodes", num_nodes), ("num_accepted", num_accepted), ("bonus", bonus)):
+        _shape(where, name, t, (b,))
+    if str(uniforms.dtype) != "torch.float32":
+        raise ValueError(f"{where}: uniforms is {uniforms.dtype}")
+    _check(lib().dartree_verify_tree(b, n, max_len, vocab, kind, _ptr(tokens), _ptr(parents), _ptr(num_nodes),
+                                     _ptr(target_logits), stride, temperature, _ptr(uniforms), _ptr(accepted),
+                                     _ptr(num_accepted), _ptr(bonus), _ptr(ws),
+                                     0 if ws is None else ws.numel() * ws.element_size(), _stream(stream)),
+           "dartree_verify_tree")
+
+
+def verify_chain(tokens, target_logits, draft_logits, temperature: float, uniforms, num_accepted, bonus, ws,
+                 num_tokens=None, stream=None) -> None:
+    """tokens [b][depth] drawn from draft_logits [b][depth][V], target_logits
+    [b][depth+1][V] (both float32 or both bfloat16), uniforms float32
+    [b][depth+1]; outputs num_accepted [b], bonus [b] (int32)."""
+    where = "verify_chain"
+    b, n = tokens.shape
+    vocab = target_logits.shape[-1]
+    _want(where, tokens=tokens, num_tokens=num_tokens, target_rows=target_logits, draft_rows=draft_logits,
+          uniforms=uniforms, num_accepted=num_accepted, bonus=bonus, ws=ws)
+    _int32(where, tokens=tokens, num_tokens=num_tokens, num_accepted=num_accepted, bonus=bonus)
+    kind, stride = _logits(where, "target_logits", target_logits, (b, n + 1, vocab))
+    if draft_logits is not None:
+        # a single draft row has no distance to the next one
+        dkind, dstride = _logits(where, "draft_logits", draft_logits, (b, n, vocab))
+        if dkind != kind or (dstride != stride and b * n > 1):
+            raise ValueError(f"{where}: draft_logits and target_logits differ in type or in the distance of their rows")
+    _shape(where, "uniforms", uniforms, (b, n + 1))
+    for name, t in (("num_tokens", num_tokens), ("num_accepted", num_accepted), ("bonus", bonus)):
+        _shape(where, name, t, (b,))
+    if str(uniforms.dtype) != "torch.float32":
+        raise ValueError(f"{where}: uniforms is {uniforms.dtype}")
+    _check(lib().dartree_verify_chain(b, n, vocab, kind, _ptr(tokens), _ptr(num_tokens), _ptr(target_logits),
+                                      _ptr(draft_logits), stride, temperature, _ptr(uniforms), _ptr(num_accepted),
+                                      _ptr(bonus), _ptr(ws), 0 if ws is None else ws.numel() * ws.element_size(),
+                                      _stream(stream)), "dartree_verify_chain")

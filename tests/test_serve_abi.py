@@ -1,0 +1,205 @@
+"""The serving entry points (include/dartree/serve.h) without a GPU: exported and
+bound, and refused arguments; the plain forms the GPU tests compare with."""
+import ctypes
+import math
+import os
+import re
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2608_13524_amd import dartree as D
+from tests import serve_ref as S
+
+HEADER = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include", "dartree", "serve.h")
+FAKE = 0x10000   # 16-byte aligned address that is never dereferenced
+byref = ctypes.byref
+
+
+def test_every_declared_symbol_is_exported_and_bound():
+    syms = sorted(set(re.findall(r"^dartree_status (dartree_\w+)\(", open(HEADER).read(), re.M)))
+    assert syms == sorted(D.SERVE_SYMBOLS) and len(syms) == 9
+    for s in syms:
+        assert hasattr(D.lib(), s)
+
+
+def cache_params(**kw):
+    p = D.CacheParams(4, 8, 128, 64, 100, 16, D.CACHE_E4M3)
+    for k, v in kw.items():
+        setattr(p, k, v)
+    return p
+
+
+@pytest.mark.parametrize("field,value,code", [
+    ("batch", 0, D.ERR_INVALID_ARG), ("heads_kv", 0, D.ERR_INVALID_ARG), ("head_dim", 0, D.ERR_INVALID_ARG),
+    ("page", 0, D.ERR_INVALID_ARG), ("num_pages", 0, D.ERR_INVALID_ARG), ("max_pages", 0, D.ERR_INVALID_ARG),
+    ("type", 2, D.ERR_INVALID_ARG), ("type", -1, D.ERR_INVALID_ARG), ("head_dim", 64, D.ERR_UNSUPPORTED),
+    ("heads_kv", 4097, D.ERR_UNSUPPORTED), ("page", 8, D.ERR_UNSUPPORTED), ("page", 48, D.ERR_UNSUPPORTED),
+    ("page", 512, D.ERR_UNSUPPORTED), ("max_pages", (1 << 24) + 1, D.ERR_UNSUPPORTED)])
+def test_cache_params_refused(field, value, code):
+    assert D.cache_validate(cache_params(**{field: value})) == code
+    assert D.cache_validate(cache_params()) == D.OK
+    assert D.cache_validate(cache_params(type=D.CACHE_BF16, page=16, max_pages=1 << 26)) == D.OK
+
+
+def test_cache_calls_refuse_before_any_launch():
+    lib, p, c = D.lib(), cache_params(), D.CacheC(FAKE, FAKE, FAKE, FAKE, FAKE)
+
+    def write(p=p, c=c, src=64, rows=16, k=FAKE, v=FAKE, stride=1024, index=FAKE, counts=FAKE, start=FAKE):
+        return lib.dartree_cache_write(p and byref(p), c and byref(c), src, rows, k, v, stride, index, counts, start, None)
+
+    bad = D.ERR_INVALID_ARG
+    assert write(p=None) == bad and write(c=None) == bad and write(p=cache_params(page=24)) == D.ERR_UNSUPPORTED
+    for i in range(5):
+        fields = [FAKE] * 5
+        for wrong in (None, FAKE + 8):
+            fields[i] = wrong
+            assert write(c=D.CacheC(*fields)) == bad
+    assert write(src=0) == bad and write(rows=0) == bad and write(index=None, src=15) == bad
+    assert write(k=None) == bad and write(v=FAKE + 2) == bad and write(stride=1016) == bad and write(stride=1028) == bad
+    assert write(index=FAKE + 4) == bad and write(counts=FAKE + 4) == bad and write(start=FAKE + 4) == bad
+    assert write(rows=1 << 26) == D.ERR_UNSUPPORTED
+
+    def read(p=p, c=c, rows=16, k=FAKE, v=FAKE, counts=None, start=None):
+        return lib.dartree_cache_read(p and byref(p), c and byref(c), rows, k, v, counts, start, None)
+
+    assert read(p=None) == bad and read(c=None) == bad and read(rows=0) == bad and read(k=None) == bad
+    assert read(v=FAKE + 8) == bad and read(counts=FAKE + 4) == bad and read(start=FAKE + 4) == bad
+    assert read(c=D.CacheC(FAKE, FAKE, None, FAKE, FAKE)) == bad
+
+
+def test_attention_refuses_before_any_launch():
+    lib, p, c = D.lib(), cache_params(), D.CacheC(FAKE, FAKE, FAKE, FAKE, FAKE)
+    base = dict(batch=4, budget=64, max_ctx=1024, heads_q=32, heads_kv=8, head_dim=128, scale=0.09)
+    need = D.tree_attention_paged_workspace_size(D.AttnParams(**base), p)
+    assert need > 0
+    for change, code in ((dict(batch=3), D.ERR_INVALID_ARG), (dict(heads_kv=4), D.ERR_INVALID_ARG),
+                         (dict(head_dim=64), D.ERR_INVALID_ARG), (dict(heads_q=33), D.ERR_INVALID_ARG),
+                         (dict(budget=0), D.ERR_INVALID_ARG), (dict(budget=4097), D.ERR_UNSUPPORTED),
+                         (dict(max_ctx=-1), D.ERR_INVALID_ARG), (dict(max_ctx=1025), D.ERR_INVALID_ARG),
+                         (dict(scale=0.0), D.ERR_INVALID_ARG), (dict(scale=math.nan), D.ERR_INVALID_ARG)):
+        with pytest.raises(D.DartreeError) as e:
+            D.tree_attention_paged_workspace_size(D.AttnParams(**{**base, **change}), p)
+        assert e.value.status == code, change
+
+    def call(q=FAKE, qs=4096, k=FAKE, v=FAKE, kvs=1024, mask=FAKE, nn=None, ctx=None, out=FAKE, ws=FAKE, n=need, c=c):
+        return lib.dartree_tree_attention_paged(byref(D.AttnParams(**base)), byref(p), byref(c), q, qs, k, v, kvs, mask, nn,
+                                                ctx, out, ws, n, None)
+
+    bad = D.ERR_INVALID_ARG
+    assert call(q=None) == bad and call(k=FAKE + 8) == bad and call(v=None) == bad and call(out=None) == bad
+    assert call(qs=4088) == bad and call(kvs=1020) == bad and call(mask=FAKE + 8) == bad
+    assert call(nn=FAKE + 4) == bad and call(ctx=FAKE + 4) == bad and call(c=D.CacheC(FAKE, FAKE, FAKE, None, FAKE)) == bad
+    assert call(ws=None) == D.ERR_WORKSPACE and call(n=need - 1) == D.ERR_WORKSPACE and call(ws=FAKE + 16) == D.ERR_WORKSPACE
+
+
+def test_verification_refuses_before_any_launch():
+    lib = D.lib()
+    need = D.verify_tree_workspace_size(2, 64, 16, 1000)
+    bad = D.ERR_INVALID_ARG
+
+    def tree(b=2, n=64, ml=16, v=1000, ty=0, ptr=(FAKE,) * 8, stride=1000, t=1.0, ws=FAKE, size=need):
+        tok, par, num, z, u, acc, cnt, bon = ptr
+        return lib.dartree_verify_tree(b, n, ml, v, ty, tok, par, num, z, stride, t, u, acc, cnt, bon, ws, size, None)
+
+    assert tree(b=0) == bad and tree(n=0) == bad and tree(ml=0) == bad and tree(v=0) == bad and tree(ty=2) == bad
+    assert tree(stride=999) == bad and tree(t=-1.0) == bad and tree(t=math.nan) == bad and tree(t=math.inf) == bad
+    assert tree(n=4097) == D.ERR_UNSUPPORTED and tree(v=(1 << 20) + 1) == D.ERR_UNSUPPORTED
+    assert tree(b=65536) == D.ERR_UNSUPPORTED
+    for i in range(8):
+        ptr = [FAKE] * 8
+        for wrong in (None, FAKE + 4):
+            ptr[i] = wrong
+            assert tree(ptr=ptr) == bad, i
+    assert tree(size=need - 1) == D.ERR_WORKSPACE and tree(ws=None) == D.ERR_WORKSPACE and tree(ws=FAKE + 16) == D.ERR_WORKSPACE
+
+    need_c = D.verify_chain_workspace_size(2, 16, 1000)
+
+    def chain(b=2, n=16, v=1000, ty=0, tok=FAKE, num=None, z=FAKE, y=FAKE, stride=1000, t=1.0, u=FAKE, cnt=FAKE, bon=FAKE,
+              ws=FAKE, size=need_c):
+        return lib.dartree_verify_chain(b, n, v, ty, tok, num, z, y, stride, t, u, cnt, bon, ws, size, None)
+
+    assert chain(b=0) == bad and chain(n=0) == bad and chain(v=0) == bad and chain(ty=-1) == bad and chain(stride=5) == bad
+    assert chain(n=65) == D.ERR_UNSUPPORTED and chain(t=-0.5) == bad
+    assert chain(tok=None) == bad and chain(num=FAKE + 4) == bad and chain(z=None) == bad and chain(y=None) == bad
+    assert chain(u=FAKE + 4) == bad and chain(cnt=None) == bad and chain(bon=None) == bad
+    assert chain(y=None, t=0.0, size=need_c - 1) == D.ERR_WORKSPACE   # at T = 0 the draft's logits may be absent
+    assert chain(ws=FAKE + 16) == D.ERR_WORKSPACE
+
+
+def test_binding_names_what_does_not_fit(monkeypatch):
+    """Shapes, types and strides that the C call cannot see."""
+    monkeypatch.setattr(torch.cuda, "is_available", lambda: False)   # no device is current: host tensors pass that check
+    p = D.CacheParams(2, 4, 128, 16, 8, 3, D.CACHE_E4M3)
+    c = D.DeviceCache.alloc(p, device="cpu")
+    x = torch.zeros(2, 5, 4, 128, dtype=torch.bfloat16)
+    i32 = dict(dtype=torch.int32)
+    with pytest.raises(ValueError, match="bfloat16"):
+        D.cache_write(p, c, x.float(), x, 5)
+    with pytest.raises(ValueError, match="neither dense"):
+        D.cache_write(p, c, x.transpose(1, 2).contiguous().transpose(1, 2), x, 5)
+    with pytest.raises(ValueError, match="equally far"):
+        D.cache_write(p, c, torch.zeros(2, 5, 8, 128, dtype=torch.bfloat16)[:, :, :4], x, 5)
+    with pytest.raises(ValueError, match="counts"):
+        D.cache_write(p, c, x, x, 5, counts=torch.zeros(3, **i32))
+    with pytest.raises(ValueError, match="int32"):
+        D.cache_write(p, c, x, x, 5, start=torch.zeros(2, dtype=torch.int64))
+    with pytest.raises(ValueError, match="table"):
+        D.cache_write(p, D.DeviceCache(c.k, c.v, c.k_exp, c.v_exp, torch.zeros(2, 4, **i32)), x, x, 5)
+    with pytest.raises(ValueError, match="cache k"):
+        D.cache_read(p, D.DeviceCache(c.k.float(), c.v, c.k_exp, c.v_exp, c.table), x, x)
+    with pytest.raises(ValueError, match="contiguous"):
+        D.cache_read(p, c, x[:, :, :2].expand(2, 5, 2, 128), x)
+    a = D.AttnParams(2, 5, 48, 8, 4, 128, 0.1)
+    q = torch.zeros(2, 5, 8, 128, dtype=torch.bfloat16)
+    with pytest.raises(ValueError, match="mask"):
+        D.tree_attention_paged(a, p, c, q, x, x, torch.zeros(2, 5, 2, dtype=torch.int64), None, q, None)
+    with pytest.raises(ValueError, match="out"):
+        D.tree_attention_paged(a, p, c, q, x, x, None, None, q[:, :4], None)
+    tok, acc, one = torch.zeros(2, 5, **i32), torch.zeros(2, 3, **i32), torch.zeros(2, **i32)
+    z, u = torch.zeros(2, 6, 10), torch.zeros(2, 6)
+    with pytest.raises(ValueError, match="target_logits"):
+        D.verify_tree(tok, tok, one, z[:, :5], 1.0, u, acc, one, one, None)
+    with pytest.raises(ValueError, match="uniforms"):
+        D.verify_tree(tok, tok, one, z, 1.0, u.double(), acc, one, one, None)
+    with pytest.raises(ValueError, match="differ"):
+        D.verify_chain(tok, z, z[:, :5].bfloat16(), 1.0, u, one, one, None)
+
+
+def test_plain_quantiser_is_e4m3():
+    """The plain quantiser against torch's cast, the 256 codes, and the bound of a rounding."""
+    rng = np.random.default_rng(5)
+    x = S.bf16(rng.normal(size=(500, 128)) * np.exp(rng.normal(size=(500, 1)) * 8))
+    q, e = S.quantise(x)
+    assert (np.abs(q).max(axis=1) <= 448).all() and (np.abs(q).max(axis=1) > 216).all()
+    cast = torch.from_numpy((x.astype(np.float64) * 2.0 ** -e[:, None]).astype(np.float32)).to(torch.float8_e4m3fn).float().numpy()
+    assert np.array_equal(cast, q)
+    held = q * 2.0 ** e[:, None]
+    # half a step of 2^-4 relative, or of the subnormals' 2^-9
+    assert (np.abs(held - x) <= np.maximum(2.0 ** -4 * np.abs(x), 2.0 ** (e[:, None] - 10.0))).all()
+    codes = S.e4m3_values()
+    bits = torch.arange(256, dtype=torch.uint8).view(torch.float8_e4m3fn).float().numpy()
+    assert np.array_equal(np.isnan(codes), np.isnan(bits)) and np.array_equal(codes[~np.isnan(codes)], bits[~np.isnan(bits)])
+
+
+@pytest.mark.parametrize("temperature", [0.0, 0.7, 1.0])
+def test_plain_verification_samples_the_target(temperature):
+    """Over many random numbers the first token (accepted or final) follows the target, for a tree
+    and for a chain: 5 standard deviations of a count of 20000 draws."""
+    rng = np.random.default_rng(6)
+    vocab, draws = 6, 20000
+    z, y = rng.normal(size=(4, vocab)) * 1.5, rng.normal(size=(1, vocab)) * 1.5
+    tokens, parents = np.array([4, 1, 2]), np.array([-1, -1, -1])
+    p = S.law(z[0], temperature)
+    count, chain = np.zeros(vocab), np.zeros(vocab)
+    q = S.law(y[0], temperature)
+    for _ in range(draws):
+        u = rng.random(4).astype(np.float32)
+        path, tok = S.verify_tree(tokens, parents, 3, z, temperature, u, 4)
+        count[tokens[path[0]] if path else tok] += 1
+        x = rng.choice(vocab, p=q)
+        n, tok = S.verify_chain(np.array([x]), 1, z[:2], y, temperature, u[:2])
+        chain[x if n else tok] += 1
+    bound = 5 * np.sqrt(draws * p * (1 - p)) + 1e-9
+    assert (np.abs(count - draws * p) <= bound).all() and (np.abs(chain - draws * p) <= bound).all()
