@@ -1,22 +1,25 @@
 // Attention of drafted trees, chains and single tokens over a paged cache.
 //
 // One pass over the keys with a running maximum and sum per query row.  Work
-// is counted in steps of 128 keys: those of a request's context, then those of
-// its tree, for every (key/value head, tile of 16 RG query rows).  The steps of
-// all requests lie on one line that the blocks share equally (or every block
-// takes one whole item, where there are many), so ragged contexts cost no idle
-// compute units; an item cut by a block's end leaves partial results, which a
-// second launch joins in block order.
+// is counted in steps of keys: those of a request's context, then those of its
+// tree, for every (key/value head, tile of query rows).  The steps of all requests
+// lie on one line that the blocks share equally (or every block takes one whole
+// item, where there are many), so ragged contexts cost no idle compute units; an
+// item cut by a block's end leaves partial results, which a second launch joins
+// in block order.
 //
-// A step's four chunks of 32 keys go to the block's four waves, and a wave works
-// from registers alone.  S^T = K Q^T: row r of the two 16-key tiles is key
+// Up to 16 query rows of a key/value head (paged_attention): a step is 128 keys,
+// a chunk of 32 for each of the block's four waves, and a wave works from
+// registers alone.  S^T = K Q^T: row r of the two 16-key tiles is key
 // 8 (r / 4) + 4 t + r % 4, which leaves lane (c = lane % 16, g = lane / 16) with
 // query c's weights of keys 8 g .. 8 g + 7 in order, the B operand of O^T = V^T P^T.
 // For V a lane reads eight dims, 8 c .. 8 c + 7, of those same keys and
 // transposes them in registers; column tile t of the product is then dims 8 c + t,
 // and a lane ends with dims 32 g .. 32 g + 31 of its query.  Keys in e4m3 become
 // bf16 on the way with their power of two applied by the conversion (exact).
-// Every key and value byte is read once per tile and never passes through LDS.
+// Every key and value byte is read once and never passes through LDS.
+//
+// More rows (paged_tiles): below.
 #include <algorithm>
 
 #include "reduce.hpp"
@@ -41,13 +44,20 @@ __device__ __forceinline__ uint32_t expand2(uint32_t w, float scale) {
   return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, HI));
 }
 
-struct Extent {   // a request's keys
+// Small arrays that a launch only reads, at addresses that are the same for all
+// lanes: scalar loads, which do not queue behind the vector loads in flight.
+typedef const __attribute__((address_space(4))) int32_t* Uniform;
+__device__ __forceinline__ Uniform uniform_array(const int32_t* p) { return (Uniform)p; }
+
+template <int STEP>
+struct Extent {   // a request's keys, in steps of STEP
   int ctx, nodes;
-  __device__ int ctx_steps() const { return (ctx + kStep - 1) / kStep; }
-  __device__ int steps() const { return max(1, ctx_steps() + (nodes + kStep - 1) / kStep); }
+  __device__ int ctx_steps() const { return (ctx + STEP - 1) / STEP; }
+  __device__ int steps() const { return max(1, ctx_steps() + (nodes + STEP - 1) / STEP); }
 };
-__device__ __forceinline__ Extent extent_of(const PagedArgs& a, int q) {
-  return Extent{a.ctx_len ? min(max(a.ctx_len[q], 0), a.max_ctx) : a.max_ctx,
+template <int STEP>
+__device__ __forceinline__ Extent<STEP> extent_of(const PagedArgs& a, int q) {
+  return Extent<STEP>{a.ctx_len ? min(max(a.ctx_len[q], 0), a.max_ctx) : a.max_ctx,
                 a.num_nodes ? min(max(a.num_nodes[q], 0), a.budget) : a.budget};
 }
 
@@ -56,21 +66,30 @@ __device__ __forceinline__ int64_t uniform64(int64_t x) {
   return int64_t(uint64_t(uint32_t(uniform(int(x))))) | (int64_t(uniform(int(x >> 32))) << 32);
 }
 
+// The same of a request that is the same for all lanes.
+template <int STEP>
+__device__ __forceinline__ Extent<STEP> extent_at(const PagedArgs& a, int q) {
+  return Extent<STEP>{a.ctx_len ? min(max(uniform_array(a.ctx_len)[q], 0), a.max_ctx) : a.max_ctx,
+                      a.num_nodes ? min(max(uniform_array(a.num_nodes)[q], 0), a.budget) : a.budget};
+}
+
 // Sum over the requests of their steps.
+template <int STEP>
 __device__ __forceinline__ int64_t all_steps(const PagedArgs& a) {
   const int lane = threadIdx.x & 63;
   int64_t total = 0;
-  for (int q0 = 0; q0 < a.batch; q0 += 64) total += wave_sum_int(q0 + lane < a.batch ? extent_of(a, q0 + lane).steps() : 0);
+  for (int q0 = 0; q0 < a.batch; q0 += 64) total += wave_sum_int(q0 + lane < a.batch ? extent_of<STEP>(a, q0 + lane).steps() : 0);
   return total;
 }
 
 // The request that step `at` of the line lies in (`per` steps of the line per
 // step of a request) and the steps before that request.
+template <int STEP>
 __device__ __forceinline__ int find_request(const PagedArgs& a, int64_t at, int per, int64_t* before) {
   const int lane = threadIdx.x & 63;
   int64_t sum = 0;
   for (int q0 = 0; q0 < a.batch; q0 += 64) {
-    const int mine = q0 + lane < a.batch ? extent_of(a, q0 + lane).steps() : 0;
+    const int mine = q0 + lane < a.batch ? extent_of<STEP>(a, q0 + lane).steps() : 0;
     int incl = mine;
 #pragma unroll
     for (int off = 1; off < 64; off <<= 1) {
@@ -87,6 +106,32 @@ __device__ __forceinline__ int find_request(const PagedArgs& a, int64_t at, int 
   }
   *before = sum * per;
   return a.batch;   // not reached for steps of the line
+}
+
+// Where a block begins on the line (or its item, where every block has a whole one).
+struct Place {
+  int q, item, step, left;   // request, item of it, step of that, steps the block has
+};
+template <int STEP>
+__device__ __forceinline__ bool place_of(const PagedArgs& a, int whole, int per, int blk, int blocks, Place* p) {
+  if (whole) {
+    p->q = blk / per;
+    p->item = blk - p->q * per;
+    p->step = 0;
+    p->left = extent_at<STEP>(a, p->q).steps();
+    return true;
+  }
+  const int64_t total = uniform64(all_steps<STEP>(a) * per);
+  const int64_t s0 = total * blk / blocks, s1 = total * (blk + 1) / blocks;
+  p->left = uniform(int(s1 - s0));
+  if (p->left <= 0) return false;
+  int64_t before;
+  p->q = find_request<STEP>(a, s0, per, &before);
+  const int steps = extent_at<STEP>(a, p->q).steps();
+  const int64_t in = s0 - before;
+  p->item = uniform(int(in / steps));
+  p->step = uniform(int(in - int64_t(p->item) * steps));
+  return true;
 }
 
 template <int RG>
@@ -208,7 +253,7 @@ __device__ __forceinline__ void chunk_step(const Chunk<RG, E8>& c, const u32x4 (
   }
 }
 
-// Partial results: slot s of part_o holds the unnormalised rows [16 RG][128] of
+// Partial results: slot s of part_o holds the unnormalised rows [ROWS][128] of
 // one cut item, part_ml their {m, l}.  Block i's first item, if cut at its
 // beginning, is slot 2 i, its last, if it begins there and is cut at its end,
 // slot 2 i + 1.
@@ -216,10 +261,10 @@ struct Parts {
   float* o;
   float* ml;
 };
-template <int RG>
+template <int ROWS>
 __device__ __forceinline__ Parts parts_of(const PagedArgs& a, int blocks) {
   float* o = static_cast<float*>(a.ws);
-  return Parts{o, o + int64_t(blocks) * 2 * 16 * RG * kHead};
+  return Parts{o, o + int64_t(blocks) * 2 * ROWS * kHead};
 }
 
 template <int RG, bool E8>
@@ -231,33 +276,15 @@ __global__ __launch_bounds__(256, RG == 1 ? 2 : 1) void paged_attention(PagedArg
   const int rows = a.budget * a.group, ntile = (rows + 16 * RG - 1) / (16 * RG);
   const int per = a.heads_kv * ntile;   // items of a request
   const int blocks = gridDim.x, blk = xcd_order(blockIdx.x, blocks);
-  const Parts parts = parts_of<RG>(a, blocks);
+  const Parts parts = parts_of<16 * RG>(a, blocks);
   const int words = 2 * ((a.budget + 63) / 64);
   const int page_size = 1 << a.c.page_log2;
 
-  int q, item, step, left;   // request, item of it, step of that, steps the block still has
-  if (whole) {
-    q = blk / per;
-    item = blk - q * per;
-    step = 0;
-    left = uniform(extent_of(a, q).steps());
-  } else {
-    const int64_t total = uniform64(all_steps(a) * per);
-    const int64_t s0 = total * blk / blocks, s1 = total * (blk + 1) / blocks;
-    left = uniform(int(s1 - s0));
-    if (left <= 0) return;
-    int64_t before;
-    q = find_request(a, s0, per, &before);
-    const int steps = uniform(extent_of(a, q).steps());
-    const int64_t in = s0 - before;
-    item = uniform(int(in / steps));
-    step = uniform(int(in - int64_t(item) * steps));
-  }
-
+  Place at;
+  if (!place_of<kStep>(a, whole, per, blk, blocks, &at)) return;
+  int q = uniform(at.q), item = uniform(at.item), step = uniform(at.step), left = uniform(at.left);
   while (left > 0) {
-    Extent ex = extent_of(a, q);
-    ex.ctx = uniform(ex.ctx);
-    ex.nodes = uniform(ex.nodes);
+    const Extent<kStep> ex = extent_at<kStep>(a, q);
     const int steps = ex.steps(), nctx = ex.ctx_steps();
     const int n = min(left, steps - step);
     const int kvh = item / ntile, rt = item - kvh * ntile;
@@ -283,7 +310,7 @@ __global__ __launch_bounds__(256, RG == 1 ? 2 : 1) void paged_attention(PagedArg
     }
 
     // context: chunk of keys kb .. kb + 31
-    const int32_t* table = a.c.table + int64_t(q) * a.c.max_pages;
+    const Uniform table = uniform_array(a.c.table) + int64_t(q) * a.c.max_pages;
     auto pages_of = [&](int kb, int& p0, int& p1) {   // pages of the chunk's halves; -1: none
       p0 = table[kb >> a.c.page_log2];
       p0 = p0 < a.c.num_pages ? p0 : -1;
@@ -297,8 +324,6 @@ __global__ __launch_bounds__(256, RG == 1 ? 2 : 1) void paged_attention(PagedArg
       if (kb >= ex.ctx) break;
       int p0, p1;
       pages_of(kb, p0, p1);
-      p0 = uniform(p0);
-      p1 = uniform(p1);
       if (p0 < 0 && p1 < 0) continue;
       const int valid = min(kChunk, ex.ctx - kb);
       uint32_t there = valid == 32 ? ~0u : (1u << valid) - 1u;
@@ -436,43 +461,437 @@ __global__ __launch_bounds__(256, RG == 1 ? 2 : 1) void paged_attention(PagedArg
   }
 }
 
+// ---------------------------------------------------------------------------
+// Many rows: a block's four waves hold 16 RG query rows each and share tiles of
+// 64 keys through LDS, in bf16 (e4m3 is converted once, as it is stored).  Tile
+// s + 1 travels in registers while tile s is multiplied, in two buffers.  A row
+// of 256 bytes keeps its 16-byte chunk c at c ^ k_place or c ^ v_place of the
+// row: K is read a row per lane, V transposed (ds_read_b64_tr_b16: lane l gets dim
+// l % 16 of keys 4 (l / 16) .. + 3).  Here the rows of S^T are the keys in order,
+// so lane group g holds the weights of keys 4 g .. + 3 of every 16, and V's
+// operand is read in that order.
+// ---------------------------------------------------------------------------
+constexpr int kTile = 64;
+constexpr int kRowBytes = 2 * kHead, kTileBytes = kTile * kRowBytes;
+#define LDS_AS __attribute__((address_space(3)))
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
+
+// XOR of the places of a row's 16-byte chunks.  K: 16 rows' reads of one chunk
+// take 16 places.  V: a transposed read takes two places of eight consecutive
+// rows, a write all places of one parity of two rows.
+__device__ __forceinline__ int k_place(int key) { return key & 15; }
+__device__ __forceinline__ int v_place(int key) { return ((key & 7) << 1) | (key & 1); }
+
+// The thread's number, computed anew where this stands: keeps what is derived
+// from it for a later part of a kernel out of the registers of the loop before.
+__device__ __forceinline__ int thread_again() {
+  int t = threadIdx.x;
+  asm volatile("" : "+v"(t));
+  return t;
+}
+
+template <int N>
+struct Index {
+  static constexpr int value = N;
+};
+
+template <int RG, bool E8>
+__global__ __launch_bounds__(256, 2) void paged_tiles(PagedArgs a, int whole) {
+  __shared__ __attribute__((aligned(16))) char smem[4 * kTileBytes];   // [buffer][K, V]
+  LDS_AS char* const lds = (LDS_AS char*)smem;
+  constexpr int kRows = 64 * RG;
+  const int lane = threadIdx.x & 63, r16 = lane & 15, g = lane >> 4;
+  const int wave = uniform(threadIdx.x >> 6);
+  const int rows = a.budget * a.group, ntile = (rows + kRows - 1) / kRows;
+  const int per = a.heads_kv * ntile;
+  const int blocks = gridDim.x, blk = xcd_order(blockIdx.x, blocks);
+  const int page_mask = (1 << a.c.page_log2) - 1;
+  const float c2 = a.scale_log2;
+
+  Place at;
+  if (!place_of<kTile>(a, whole, per, blk, blocks, &at)) return;
+  int q = uniform(at.q), item = uniform(at.item), step = uniform(at.step), left = uniform(at.left);
+
+  while (left > 0) {
+    const Extent<kTile> ex = extent_at<kTile>(a, q);
+    const int steps = ex.steps(), nctx = ex.ctx_steps();
+    const int n = min(left, steps - step), last = step + n;
+    const int kvh = item / ntile, rt = item - kvh * ntile;
+
+    u32x4 qf[RG][4];
+    float m[RG], l[RG], bar[RG], ref[RG];   // bar: a score above it moves the reference m; ref = -m c2
+    f32x4 o[RG][8];
+    {
+      const int tid = thread_again();
+#pragma unroll
+      for (int r = 0; r < RG; ++r) {
+        const int row = min(rt * kRows + (tid >> 6) * (16 * RG) + r * 16 + (tid & 15), rows - 1);   // past the end: the last row, never stored
+        const int node = row / a.group;
+        const uint16_t* qp = a.q + (int64_t(q) * a.budget + node) * a.q_stride + (kvh * a.group + row - node * a.group) * kHead;
+#pragma unroll
+        for (int ks = 0; ks < 4; ++ks) qf[r][ks] = *reinterpret_cast<const u32x4*>(qp + 32 * ks + 8 * ((tid & 63) >> 4));
+        m[r] = bar[r] = -INFINITY;
+        l[r] = ref[r] = 0.f;
+#pragma unroll
+        for (int t = 0; t < 8; ++t) o[r][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+      }
+    }
+
+    // operand addresses within a buffer, the same for all tiles
+    int ka[4], va[8];
+    const int vr = 4 * g + (r16 >> 2);
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks) ka[ks] = r16 * kRowBytes + ((4 * ks + g) ^ k_place(r16)) * 16;
+#pragma unroll
+    for (int t = 0; t < 8; ++t)
+      va[t] = kTileBytes + vr * kRowBytes + ((2 * t + ((r16 & 3) >> 1)) ^ v_place(vr)) * 16 + (r16 & 1) * 8;
+
+    // scores of 32 keys, half c of the tile in buffer B
+    auto scores = [&](auto B, auto C, f32x4 (&sc)[RG][2]) __attribute__((always_inline)) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+#pragma unroll
+        for (int r = 0; r < RG; ++r) sc[r][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int ks = 0; ks < 4; ++ks) {
+          const u32x4 kf = *reinterpret_cast<const LDS_AS u32x4*>(
+              lds + ka[ks] + (B.value * 2 * kTileBytes + (C.value * 32 + t * 16) * kRowBytes));
+#pragma unroll
+          for (int r = 0; r < RG; ++r) sc[r][t] = mfma16(kf, qf[r][ks], sc[r][t]);
+        }
+      }
+    };
+    // unseen keys out; the reference of a row moves as in chunk_step, one test for all rows
+    auto settle = [&](bool masked, const uint32_t (&vis)[RG], f32x4 (&sc)[RG][2]) __attribute__((always_inline)) {
+      if (masked) {
+#pragma unroll
+        for (int r = 0; r < RG; ++r) {
+          const uint32_t bits = vis[r] >> (4 * g);
+#pragma unroll
+          for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              if (!((bits >> (16 * t + i)) & 1u)) sc[r][t][i] = -INFINITY;
+        }
+      }
+      float top[RG];
+      bool grow = false;
+#pragma unroll
+      for (int r = 0; r < RG; ++r) {
+        top[r] = sc[r][0][0];
+#pragma unroll
+        for (int x = 1; x < 8; ++x) top[r] = fmaxf(top[r], sc[r][x >> 2][x & 3]);
+        grow |= top[r] > bar[r];
+      }
+      if (__any(grow)) {
+#pragma unroll
+        for (int r = 0; r < RG; ++r) {
+          float x = fmaxf(top[r], __shfl_xor(top[r], 16));
+          x = fmaxf(x, __shfl_xor(x, 32));
+          if (x <= bar[r]) x = m[r];
+          const float f = __builtin_amdgcn_exp2f((m[r] - (x == -INFINITY ? 0.f : x)) * c2);
+          l[r] *= f;
+#pragma unroll
+          for (int t = 0; t < 8; ++t) o[r][t] *= f;
+          m[r] = x;
+          bar[r] = x + 8.f / c2;
+          ref[r] = x == -INFINITY ? 0.f : -x * c2;
+        }
+      }
+    };
+    auto weights = [&](const f32x4 (&sc)[RG][2], u32x4 (&p)[RG]) __attribute__((always_inline)) {
+#pragma unroll
+      for (int r = 0; r < RG; ++r) {
+        bf16x8 w;
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float e = __builtin_amdgcn_exp2f(fmaf(sc[r][t][i], c2, ref[r]));
+            l[r] += e;
+            w[4 * t + i] = __bf16(e);
+          }
+        p[r] = __builtin_bit_cast(u32x4, w);
+      }
+    };
+    auto values = [&](auto B, auto C, const u32x4 (&p)[RG]) __attribute__((always_inline)) {
+#pragma unroll
+      for (int t = 0; t < 8; ++t) {
+        const LDS_AS char* at = lds + va[t] + (B.value * 2 * kTileBytes + C.value * 32 * kRowBytes);
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4*)at);
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4*)(at + 16 * kRowBytes));
+        const u32x4 vf = __builtin_bit_cast(u32x4, s16x8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]});
+#pragma unroll
+        for (int r = 0; r < RG; ++r) o[r][t] = mfma16(vf, p[r], o[r][t]);
+      }
+    };
+
+    // Tiles first .. end - 1 of one source.  fetch(s): a thread's share of tile s
+    // into registers; store(B): the fetched tile to buffer B, returning which of
+    // its keys are there (one that is not has zeros for values: 0 * NaN is NaN);
+    // sees(s, r, there): what row group r sees of the keys that are.
+    auto sweep = [&](const int first, const int end, auto&& fetch, auto&& store, auto&& sees, const bool tree) __attribute__((always_inline)) {
+      if (first >= end) return;
+      fetch(first);
+      uint64_t there = store(Index<0>());
+      if (first + 1 < end) fetch(first + 1);
+      __syncthreads();
+      f32x4 sa[RG][2], sb[RG][2];
+      u32x4 p[RG];
+      uint32_t seen[2][RG];
+      scores(Index<0>(), Index<0>(), sa);
+      auto tile = [&](auto B, int s) __attribute__((always_inline)) {
+        const Index<1 - B.value> other;
+        const bool masked = tree || there != ~0ull;
+        if (masked) {
+#pragma unroll
+          for (int r = 0; r < RG; ++r) {
+            const uint64_t vis = sees(s, r, there);
+            seen[0][r] = uint32_t(vis);
+            seen[1][r] = uint32_t(vis >> 32);
+          }
+        }
+        // the products of the next 32 keys' scores run beside the exponentials of these
+        settle(masked, seen[0], sa);
+        scores(B, Index<1>(), sb);
+        weights(sa, p);
+        values(B, Index<0>(), p);
+        settle(masked, seen[1], sb);
+        if (s + 1 < end) {
+          there = store(other);
+          if (s + 2 < end) fetch(s + 2);
+        }
+        __syncthreads();
+        scores(other, Index<0>(), sa);   // after the last tile: not used
+        weights(sb, p);
+        values(B, Index<1>(), p);
+        __syncthreads();   // both buffers are free again
+      };
+#pragma unroll 1
+      for (int s = first; s < end; s += 2) {
+        tile(Index<0>(), s);
+        if (s + 1 < end) tile(Index<1>(), s + 1);
+      }
+    };
+
+    {   // the context
+      const int32_t* table = a.c.table + int64_t(q) * a.c.max_pages;
+      constexpr int kShares = E8 ? 2 : 4;
+      u32x4 kx[kShares], vx[kShares];
+      uint32_t ke[2], ve[2];
+      uint64_t in_flight = 0;
+      int page;   // lane i % 4: the page of the i-th 16 keys of the tile to fetch next
+      auto look_up = [&](int s) __attribute__((always_inline)) {
+        page = table[min(s * kTile + 16 * (thread_again() & 3), ex.ctx - 1) >> a.c.page_log2];
+      };
+      // a wave's keys of a share lie in one group of 16, so in one page: in e4m3
+      // eight rows of 128 bytes, keys 32 i + 8 wave ..; in bf16 four of 256, 16 i + 4 wave ..
+      auto fetch = [&](int s) __attribute__((always_inline)) {
+        const int kb = s * kTile, valid = min(kTile, ex.ctx - kb);
+        in_flight = valid == 64 ? ~0ull : (1ull << valid) - 1;
+        int pg[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          pg[i] = __builtin_amdgcn_readlane(page, i);
+          if (uint32_t(pg[i]) >= uint32_t(a.c.num_pages)) {
+            in_flight &= ~(0xFFFFull << (16 * i));
+            pg[i] = 0;   // any page: what is read is not used
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < kShares; ++i) {
+          const int64_t of = !E8 ? pg[i] : wave < 2 ? pg[2 * i & 3] : pg[(2 * i + 1) & 3];
+          const int64_t row0 = ((of * a.heads_kv + kvh) << a.c.page_log2) + ((kb + (E8 ? 32 * i + 8 * wave : 16 * i + 4 * wave)) & page_mask);
+          const int64_t byte0 = row0 * (E8 ? kHead : 2 * kHead);
+          kx[i] = *reinterpret_cast<const u32x4*>(static_cast<const char*>(a.c.k) + byte0 + 16 * lane);
+          vx[i] = *reinterpret_cast<const u32x4*>(static_cast<const char*>(a.c.v) + byte0 + 16 * lane);
+          if constexpr (E8) {
+            ke[i] = a.c.k_exp[row0 + (lane >> 3)];
+            ve[i] = a.c.v_exp[row0 + (lane >> 3)];
+          }
+        }
+        look_up(s + 1);
+      };
+      auto store = [&](auto B) __attribute__((always_inline)) -> uint64_t {
+        const uint64_t there = in_flight;
+        const u32x4 zero{0, 0, 0, 0};
+        LDS_AS char* const kt = lds + B.value * 2 * kTileBytes;
+#pragma unroll
+        for (int i = 0; i < kShares; ++i) {
+          const int key = E8 ? 32 * i + 8 * wave + (lane >> 3) : 16 * i + 4 * wave + g;
+          const bool gone = there != ~0ull && !((there >> key) & 1);
+          if (gone) vx[i] = zero;
+          if constexpr (E8) {
+            const float sk = __uint_as_float(ke[i] << 23), sv = gone ? 1.f : __uint_as_float(ve[i] << 23);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              const int c = 2 * (lane & 7) + h;
+              *reinterpret_cast<LDS_AS u32x4*>(kt + key * kRowBytes + (c ^ k_place(key)) * 16) =
+                  u32x4{expand2<false>(kx[i][2 * h], sk), expand2<true>(kx[i][2 * h], sk), expand2<false>(kx[i][2 * h + 1], sk),
+                        expand2<true>(kx[i][2 * h + 1], sk)};
+              *reinterpret_cast<LDS_AS u32x4*>(kt + kTileBytes + key * kRowBytes + (c ^ v_place(key)) * 16) =
+                  u32x4{expand2<false>(vx[i][2 * h], sv), expand2<true>(vx[i][2 * h], sv), expand2<false>(vx[i][2 * h + 1], sv),
+                        expand2<true>(vx[i][2 * h + 1], sv)};
+            }
+          } else {
+            *reinterpret_cast<LDS_AS u32x4*>(kt + key * kRowBytes + (r16 ^ k_place(key)) * 16) = kx[i];
+            *reinterpret_cast<LDS_AS u32x4*>(kt + kTileBytes + key * kRowBytes + (r16 ^ v_place(key)) * 16) = vx[i];
+          }
+        }
+        return there;
+      };
+      if (step < min(last, nctx)) look_up(step);
+      sweep(step, min(last, nctx), fetch, store, [&](int, int, uint64_t there) { return there; }, false);
+    }
+    const int tid = thread_again();
+    int node[RG], row[RG];
+#pragma unroll
+    for (int r = 0; r < RG; ++r) {
+      row[r] = rt * kRows + (tid >> 6) * (16 * RG) + r * 16 + (tid & 15);
+      node[r] = min(row[r], rows - 1) / a.group;
+    }
+    {   // the tree's own keys
+      const int words = (a.budget + 63) / 64;
+      const int key0 = tid >> 4, c = tid & 15;
+      u32x4 kx[4], vx[4];
+      uint64_t in_flight = 0, next_seen[RG], seen[RG];   // mask words of the tile in flight, of the stored one
+      auto fetch = [&](int s) __attribute__((always_inline)) {
+        const int kb = (s - nctx) * kTile, valid = min(kTile, ex.nodes - kb);   // 0 where a request has no keys at all
+        in_flight = valid >= 64 ? ~0ull : (1ull << max(valid, 0)) - 1;
+        if (a.mask) {
+#pragma unroll
+          for (int r = 0; r < RG; ++r)
+            next_seen[r] = a.mask[(int64_t(q) * a.budget + node[r]) * words + min(s - nctx, words - 1)];
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int key = min(kb + 16 * i + key0, a.budget - 1);
+          const int64_t off = (int64_t(q) * a.budget + key) * a.kv_stride + kvh * kHead + 8 * c;
+          kx[i] = *reinterpret_cast<const u32x4*>(a.k_tree + off);
+          vx[i] = *reinterpret_cast<const u32x4*>(a.v_tree + off);
+        }
+      };
+      auto store = [&](auto B) __attribute__((always_inline)) -> uint64_t {
+        const u32x4 zero{0, 0, 0, 0};
+        LDS_AS char* const kt = lds + B.value * 2 * kTileBytes;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int key = 16 * i + key0;
+          *reinterpret_cast<LDS_AS u32x4*>(kt + key * kRowBytes + (c ^ k_place(key)) * 16) = kx[i];
+          *reinterpret_cast<LDS_AS u32x4*>(kt + kTileBytes + key * kRowBytes + (c ^ v_place(key)) * 16) =
+              (in_flight >> key) & 1 ? vx[i] : zero;
+        }
+#pragma unroll
+        for (int r = 0; r < RG; ++r) seen[r] = next_seen[r];
+        return in_flight;
+      };
+      auto sees = [&](int s, int r, uint64_t there) __attribute__((always_inline)) -> uint64_t {
+        if (a.mask) return there & seen[r];
+        const int d = node[r] - (s - nctx) * kTile;   // a chain's node sees keys up to its own
+        return there & (d < 0 ? 0ull : d >= 63 ? ~0ull : (2ull << d) - 1);
+      };
+      sweep(max(step, nctx), last, fetch, store, sees, true);
+    }
+
+    const bool direct = n == steps;
+    const int slot = 2 * blk + (step > 0 ? 0 : 1);
+    const int ge = (tid & 63) >> 4;
+#pragma unroll
+    for (int r = 0; r < RG; ++r) {
+      float total = l[r];
+      total += __shfl_xor(total, 16);
+      total += __shfl_xor(total, 32);
+      if (row[r] >= rows) continue;
+      if (direct) {
+        const float inv = total > 0.f ? 1.f / total : 0.f;   // a row that sees nothing is zero
+        uint16_t* op = a.out + ((int64_t(q) * a.budget + node[r]) * a.heads_q + kvh * a.group + row[r] - node[r] * a.group) * kHead;
+        typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+#pragma unroll
+        for (int t = 0; t < 8; ++t)
+          *reinterpret_cast<bf16x4*>(op + 16 * t + 4 * ge) =
+              bf16x4{__bf16(o[r][t][0] * inv), __bf16(o[r][t][1] * inv), __bf16(o[r][t][2] * inv), __bf16(o[r][t][3] * inv)};
+      } else {
+        const Parts parts = parts_of<kRows>(a, blocks);
+        const int64_t lr = int64_t(slot) * kRows + row[r] - rt * kRows;
+#pragma unroll
+        for (int t = 0; t < 8; ++t) *reinterpret_cast<f32x4*>(parts.o + lr * kHead + 16 * t + 4 * ge) = o[r][t];
+        if (ge == 0) {
+          parts.ml[lr * 2] = m[r];
+          parts.ml[lr * 2 + 1] = total;
+        }
+      }
+    }
+
+    left -= n;
+    step = 0;
+    if (++item == per) {
+      item = 0;
+      ++q;
+    }
+  }
+}
+
 // Join the partial results of the items that were cut: block (item, eight of its
-// rows), 32 lanes per row.
-template <int RG>
-__global__ __launch_bounds__(256) void paged_attention_join(PagedArgs a, int blocks) {
-  const int rows = a.budget * a.group, ntile = (rows + 16 * RG - 1) / (16 * RG), per = a.heads_kv * ntile;
-  const int part = blockIdx.x % (2 * RG);
-  const int it = blockIdx.x / (2 * RG);
+// rows), 32 lanes per row.  Eight blocks' results are loaded together and folded
+// in block order.
+template <int ROWS, int STEP>
+__global__ __launch_bounds__(256) void paged_join(PagedArgs a, int blocks) {
+  const int rows = a.budget * a.group, ntile = (rows + ROWS - 1) / ROWS, per = a.heads_kv * ntile;
+  const int part = blockIdx.x % (ROWS / 8);
+  const int it = blockIdx.x / (ROWS / 8);
   const int q = it / per, item = it - q * per;
   const int lane = threadIdx.x & 63;
   int64_t total = 0, before = 0;
   for (int q0 = 0; q0 < a.batch; q0 += 64) {
-    const int mine = q0 + lane < a.batch ? extent_of(a, q0 + lane).steps() : 0;
+    const int mine = q0 + lane < a.batch ? extent_of<STEP>(a, q0 + lane).steps() : 0;
     total += wave_sum_int(mine);
     before += wave_sum_int(q0 + lane < q ? mine : 0);
   }
-  const int steps = uniform(extent_of(a, q).steps());
+  const int steps = extent_at<STEP>(a, q).steps();
   total = uniform64(total * per);
   const int64_t first = uniform64(before * per + int64_t(item) * steps);
   const int b0 = int(((first + 1) * blocks - 1) / total), b1 = int(((first + steps) * blocks - 1) / total);
   if (b0 == b1) return;
   const int kvh = item / ntile, rt = item - kvh * ntile;
-  const int lr = part * 8 + (threadIdx.x >> 5), row = rt * 16 * RG + lr, d = 4 * (threadIdx.x & 31);
+  const int lr = part * 8 + (threadIdx.x >> 5), row = rt * ROWS + lr, d = 4 * (threadIdx.x & 31);
   if (row >= rows) return;
-  const Parts parts = parts_of<RG>(a, blocks);
+  const Parts parts = parts_of<ROWS>(a, blocks);
   float M = -INFINITY, L = 0.f;
   f32x4 acc{0.f, 0.f, 0.f, 0.f};
-  for (int b = b0; b <= b1; ++b) {
-    if (total * b / blocks == total * (b + 1) / blocks) continue;   // fewer steps than blocks: one without any
-    const int64_t p = int64_t(2 * b + (b == b0 ? 1 : 0)) * 16 * RG + lr;
-    const float m = parts.ml[2 * p], l = parts.ml[2 * p + 1];
-    const f32x4 o = *reinterpret_cast<const f32x4*>(parts.o + p * kHead + d);
-    if (m == -INFINITY) continue;
-    const float top = fmaxf(M, m);
-    const float f = __builtin_amdgcn_exp2f((M - top) * a.scale_log2), w = __builtin_amdgcn_exp2f((m - top) * a.scale_log2);
-    L = L * f + l * w;
-    acc = acc * f + o * w;
+  constexpr int B = 8;
+  typedef float f32x2 __attribute__((ext_vector_type(2)));
+  const bool sparse = total < blocks;   // fewer steps than blocks: some have none
+  for (int c0 = b0; c0 <= b1; c0 += B) {
+    f32x2 ml[B];
+    f32x4 o[B];
+#pragma unroll
+    for (int i = 0; i < B; ++i) {
+      const int b = min(c0 + i, b1);
+      const int64_t p = int64_t(2 * b + (b == b0 ? 1 : 0)) * ROWS + lr;
+      ml[i] = *reinterpret_cast<const f32x2*>(parts.ml + 2 * p);
+      o[i] = *reinterpret_cast<const f32x4*>(parts.o + p * kHead + d);
+    }
+    float top = M;
+    bool use[B];
+#pragma unroll
+    for (int i = 0; i < B; ++i) {
+      const int b = c0 + i;
+      use[i] = b <= b1 && !(sparse && total * b / blocks == total * (b + 1) / blocks) && ml[i][0] != -INFINITY;
+      if (use[i]) top = fmaxf(top, ml[i][0]);
+    }
+    if (top == -INFINITY) continue;
+    const float f = __builtin_amdgcn_exp2f((M - top) * a.scale_log2);
+    L *= f;
+    acc *= f;
     M = top;
+#pragma unroll
+    for (int i = 0; i < B; ++i)
+      if (use[i]) {
+        const float w = __builtin_amdgcn_exp2f((ml[i][0] - top) * a.scale_log2);
+        L += w * ml[i][1];
+        acc += o[i] * w;
+      }
   }
   const float inv = L > 0.f ? 1.f / L : 0.f;
   const int node = row / a.group;
@@ -481,30 +900,36 @@ __global__ __launch_bounds__(256) void paged_attention_join(PagedArgs a, int blo
   *reinterpret_cast<bf16x4*>(out) = bf16x4{__bf16(acc[0] * inv), __bf16(acc[1] * inv), __bf16(acc[2] * inv), __bf16(acc[3] * inv)};
 }
 
-// Row groups of 16 per tile, and the blocks of a launch.
+// Which kernel (tiles: paged_tiles, else paged_attention), its tile's query rows
+// and the blocks of a launch: as many as the chip holds, sharing the line of
+// steps, or one per item where there are plenty.
 struct Plan {
-  int rg, blocks, whole;
+  int tiles, rows, blocks, whole;
   int64_t items;
 };
 Plan plan_of(int batch, int budget, int max_ctx, int heads_q, int heads_kv) {
+  constexpr int kResident = 512;   // two blocks a compute unit
   const int rows = budget * (heads_q / heads_kv);
   Plan p{};
-  p.rg = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
-  p.items = int64_t(batch) * heads_kv * ((rows + 16 * p.rg - 1) / (16 * p.rg));
-  const int resident = p.rg == 1 ? 512 : 256;
-  p.whole = p.items >= 4 * resident;
-  const int64_t steps = std::max(1, (max_ctx + kStep - 1) / kStep + (budget + kStep - 1) / kStep);
-  p.blocks = int(p.whole ? p.items : std::min<int64_t>(resident, p.items * steps));
+  p.tiles = rows > 16;
+  const int step = p.tiles ? kTile : kStep;
+  const int64_t steps = std::max(1, (max_ctx + step - 1) / step + (budget + step - 1) / step);
+  const int64_t heads = int64_t(batch) * heads_kv;
+  // 128 rows a tile double a tile's products per byte from LDS, and a cut item's
+  // partial results; worth it where blocks take eight steps and more
+  p.rows = !p.tiles ? 16 : rows <= 64 || heads * ((rows + 127) / 128) * steps < 8 * kResident ? 64 : 128;
+  p.items = heads * ((rows + p.rows - 1) / p.rows);
+  p.whole = p.items >= 4 * kResident;
+  p.blocks = int(p.whole ? p.items : std::min<int64_t>(kResident, p.items * steps));
   return p;
 }
 
-template <int RG>
-hipError_t launch(const PagedArgs& a, const Plan& p, hipStream_t s) {
-  if (a.eight) hipLaunchKernelGGL((paged_attention<RG, true>), dim3(p.blocks), dim3(256), 0, s, a, p.whole);
-  else hipLaunchKernelGGL((paged_attention<RG, false>), dim3(p.blocks), dim3(256), 0, s, a, p.whole);
+template <int ROWS, int STEP, typename K>
+hipError_t launch(K* kernel, const PagedArgs& a, const Plan& p, hipStream_t s) {
+  hipLaunchKernelGGL(kernel, dim3(p.blocks), dim3(256), 0, s, a, p.whole);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.whole) return e;
-  hipLaunchKernelGGL(paged_attention_join<RG>, dim3(unsigned(p.items * 2 * RG)), dim3(256), 0, s, a, p.blocks);
+  hipLaunchKernelGGL((paged_join<ROWS, STEP>), dim3(unsigned(p.items * (ROWS / 8))), dim3(256), 0, s, a, p.blocks);
   return hipGetLastError();
 }
 
@@ -512,12 +937,14 @@ hipError_t launch(const PagedArgs& a, const Plan& p, hipStream_t s) {
 
 size_t paged_attention_workspace(int batch, int budget, int max_ctx, int heads_q, int heads_kv, int) {
   const Plan p = plan_of(batch, budget, max_ctx, heads_q, heads_kv);
-  return p.whole ? 0 : size_t(p.blocks) * 2 * 16 * p.rg * (kHead + 2) * sizeof(float);
+  return p.whole ? 0 : size_t(p.blocks) * 2 * p.rows * (kHead + 2) * sizeof(float);
 }
 
 hipError_t launch_paged_attention(const PagedArgs& a, hipStream_t s) {
   const Plan p = plan_of(a.batch, a.budget, a.max_ctx, a.heads_q, a.heads_kv);
-  return p.rg == 1 ? launch<1>(a, p, s) : p.rg == 2 ? launch<2>(a, p, s) : launch<4>(a, p, s);
+  if (!p.tiles) return a.eight ? launch<16, kStep>(paged_attention<1, true>, a, p, s) : launch<16, kStep>(paged_attention<1, false>, a, p, s);
+  if (p.rows == 64) return a.eight ? launch<64, kTile>(paged_tiles<1, true>, a, p, s) : launch<64, kTile>(paged_tiles<1, false>, a, p, s);
+  return a.eight ? launch<128, kTile>(paged_tiles<2, true>, a, p, s) : launch<128, kTile>(paged_tiles<2, false>, a, p, s);
 }
 
 }  // namespace dartree

@@ -570,47 +570,65 @@ def tree_attention(p: AttnParams, q, k_ctx, v_ctx, k_tree, v_tree, mask, ctx_len
 # ---------------------------------------------------------------------------
 # Serving: a paged cache, attention over it, verification (dartree/serve.h)
 # ---------------------------------------------------------------------------
-def _want(where: str, **tensors) -> None:
-    """Each tensor (None: not given) on the current device and, unless its name
-    ends in _rows (checked by its caller), dense; ValueError otherwise."""
+def _place(stream):
+    """(index of the current device, stream handle); device -1 before the GPU has been used."""
     import torch
-    device = torch.cuda.current_device() if torch.cuda.is_available() else -1
-    for name, t in tensors.items():
-        if t is None:
-            continue
-        if t.get_device() != device:
-            raise ValueError(f"{where}: {name} is on {t.device}, not on the current device")
-        if not name.endswith("_rows") and not t.is_contiguous():
-            raise ValueError(f"{where}: {name} is not contiguous")
+    if not torch.cuda.is_initialized():
+        return -1, None
+    if stream is None:
+        s = torch.cuda.current_stream()
+        return s.device_index, s.cuda_stream
+    return torch.cuda.current_device(), getattr(stream, "cuda_stream", stream)
 
 
-def _row_stride(where: str, name: str, t) -> int:
-    """Elements between the rows of t [b][rows][heads][128]: heads are dense,
-    rows may be apart, requests follow each other."""
-    b, rows, heads, dim = t.shape
-    st = t.stride()
-    if st[3] != 1 or (heads > 1 and st[2] != dim) or (b > 1 and st[0] != rows * st[1]):
+def _refuse(where: str, name: str, t, dtypes: tuple, shape: tuple, device: int):
+    """ValueError that names what does not fit (called where something does not)."""
+    if t.dtype not in dtypes:
+        raise ValueError(f"{where}: {name} is {t.dtype}, not {' or '.join(str(d) for d in dtypes)}")
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{where}: {name} is {tuple(t.shape)}, not {tuple(shape)}")
+    if t.get_device() != device:
+        raise ValueError(f"{where}: {name} is on {t.device}, not on the current device")
+    raise ValueError(f"{where}: {name} is not contiguous")
+
+
+def _dense(where: str, name: str, t, dtype, shape: tuple, device: int):
+    """Address of a dense tensor of this type and shape on this device (None for None)."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != device or not t.is_contiguous():
+        _refuse(where, name, t, (dtype,), shape, device)
+    return t.data_ptr()
+
+
+def _rows(where: str, name: str, t, dtypes: tuple, shape: tuple, device: int):
+    """(address, elements between rows) of [b][rows]... whose rows may be apart:
+    each row is dense and requests follow each other."""
+    if t.dtype not in dtypes or t.shape != shape or t.get_device() != device:
+        _refuse(where, name, t, dtypes, shape, device)
+    row = shape[2] if len(shape) == 3 else shape[2] * shape[3]
+    if t.is_contiguous():
+        return t.data_ptr(), row
+    b, rows, st = shape[0], shape[1], t.stride()
+    dense = all(n == 1 or s == w for n, s, w in zip(shape[2:], st[2:], (shape[-1], 1)[-(len(shape) - 2):]))
+    step = st[1] if rows > 1 else st[0] if b > 1 else row
+    if not dense or (b > 1 and rows > 1 and st[0] != rows * step):
         raise ValueError(f"{where}: {name} is neither dense nor rows of a wider tensor")
-    if rows > 1:
-        return st[1]
-    return st[0] if b > 1 else heads * dim
+    return t.data_ptr(), step
 
 
-def _bf16(where: str, **tensors) -> None:
-    for name, t in tensors.items():
-        if str(t.dtype) != "torch.bfloat16":
-            raise ValueError(f"{where}: {name} is {t.dtype}, not bfloat16")
+def _workspace(where: str, ws, device: int):
+    """(address, bytes) of a workspace."""
+    if ws is None:
+        return None, 0
+    if ws.get_device() != device or not ws.is_contiguous():
+        _refuse(where, "ws", ws, (ws.dtype,), ws.shape, device)
+    return ws.data_ptr(), ws.numel() * ws.element_size()
 
 
-def _int32(where: str, **tensors) -> None:
-    for name, t in tensors.items():
-        if t is not None and str(t.dtype) != "torch.int32":
-            raise ValueError(f"{where}: {name} is {t.dtype}, not int32")
-
-
-def _shape(where: str, name: str, t, want: tuple) -> None:
-    if t is not None and tuple(t.shape) != want:
-        raise ValueError(f"{where}: {name} is {tuple(t.shape)}, not {want}")
+def _on_device(where: str, device: int) -> None:
+    if device < 0:
+        raise ValueError(f"{where}: the tensors are not on a GPU")
 
 
 @dataclasses.dataclass
@@ -639,22 +657,18 @@ class DeviceCache:
         return DeviceCache(pages(), pages(), exps(), exps(),
                            torch.full((p.batch, p.max_pages), -1, dtype=torch.int32, device=device))
 
-    def check(self, p: CacheParams, where: str) -> None:
+    def checked(self, p: CacheParams, where: str, device: int) -> CacheC:
+        """The C struct, once every tensor fits `p` (ValueError otherwise)."""
+        import torch
         shape = (p.num_pages, p.heads_kv, p.page)
         eight = p.type == CACHE_E4M3
-        for name in ("k", "v"):
-            t = getattr(self, name)
-            _shape(where, name, t, (*shape, p.head_dim))
-            if t.element_size() != (1 if eight else 2):
-                raise ValueError(f"{where}: cache {name} is {t.dtype}")
-            if eight:
-                e = getattr(self, name + "_exp")
-                _shape(where, name + "_exp", e, shape)
-                if e is not None and e.element_size() != 1:
-                    raise ValueError(f"{where}: cache {name}_exp is {e.dtype}")
-        _shape(where, "table", self.table, (p.batch, p.max_pages))
-        _int32(where, table=self.table)
-        _want(where, k=self.k, v=self.v, k_exp=self.k_exp, v_exp=self.v_exp, table=self.table)
+        held = torch.float8_e4m3fn if eight else torch.bfloat16
+        pages = (*shape, p.head_dim)
+        return CacheC(_dense(where, "cache k", self.k, held, pages, device),
+                      _dense(where, "cache v", self.v, held, pages, device),
+                      _dense(where, "k_exp", self.k_exp, torch.uint8, shape, device) if eight else None,
+                      _dense(where, "v_exp", self.v_exp, torch.uint8, shape, device) if eight else None,
+                      _dense(where, "table", self.table, torch.int32, (p.batch, p.max_pages), device))
 
 
 def cache_validate(p: CacheParams) -> int:
@@ -666,41 +680,39 @@ def cache_write(p: CacheParams, cache: DeviceCache, k, v, rows: int, index=None,
     """Position start[q] + i of request q, i < counts[q] <= rows, takes row
     index[q][i] (None: i) of k and v [b][source_rows][heads_kv][128] bfloat16
     (rows of a wider tensor are taken as they are)."""
-    where = "cache_write"
-    cache.check(p, where)
-    _want(where, k_rows=k, v_rows=v, index=index, counts=counts, start=start)
-    _bf16(where, k=k, v=v)
-    _int32(where, index=index, counts=counts, start=start)
-    src = k.shape[1]
-    for name, t in (("k", k), ("v", v)):
-        _shape(where, name, t, (p.batch, src, p.heads_kv, p.head_dim))
-    _shape(where, "index", index, (p.batch, rows))
-    _shape(where, "counts", counts, (p.batch,))
-    _shape(where, "start", start, (p.batch,))
-    stride = _row_stride(where, "k", k)
-    if _row_stride(where, "v", v) != stride:
+    import torch
+    where, i32 = "cache_write", torch.int32
+    device, st = _place(stream)
+    cc = cache.checked(p, where, device)
+    b, src = p.batch, k.shape[1]
+    shape = (b, src, p.heads_kv, p.head_dim)
+    kp, step = _rows(where, "k", k, (torch.bfloat16,), shape, device)
+    vp, vstep = _rows(where, "v", v, (torch.bfloat16,), shape, device)
+    if step != vstep:
         raise ValueError(f"{where}: the rows of k and v are not equally far apart")
-    cc = cache.c()
-    _check(lib().dartree_cache_write(ctypes.byref(p), ctypes.byref(cc), src, rows, _ptr(k), _ptr(v), stride, _ptr(index),
-                                     _ptr(counts), _ptr(start), _stream(stream)), "dartree_cache_write")
+    ip = _dense(where, "index", index, i32, (b, rows), device)
+    cp = _dense(where, "counts", counts, i32, (b,), device)
+    sp = _dense(where, "start", start, i32, (b,), device)
+    _on_device(where, device)
+    _check(lib().dartree_cache_write(ctypes.byref(p), ctypes.byref(cc), src, rows, kp, vp, step, ip, cp, sp, st),
+           "dartree_cache_write")
 
 
 def cache_read(p: CacheParams, cache: DeviceCache, k, v, counts=None, start=None, stream=None) -> None:
     """Rows i < counts[q] of k, v [b][rows][heads_kv][128] bfloat16 take the
     cache's positions start[q] + i."""
-    where = "cache_read"
-    cache.check(p, where)
-    _want(where, k=k, v=v, counts=counts, start=start)
-    _bf16(where, k=k, v=v)
-    _int32(where, counts=counts, start=start)
-    rows = k.shape[1]
-    for name, t in (("k", k), ("v", v)):
-        _shape(where, name, t, (p.batch, rows, p.heads_kv, p.head_dim))
-    _shape(where, "counts", counts, (p.batch,))
-    _shape(where, "start", start, (p.batch,))
-    cc = cache.c()
-    _check(lib().dartree_cache_read(ctypes.byref(p), ctypes.byref(cc), rows, _ptr(k), _ptr(v), _ptr(counts), _ptr(start),
-                                    _stream(stream)), "dartree_cache_read")
+    import torch
+    where, i32 = "cache_read", torch.int32
+    device, st = _place(stream)
+    cc = cache.checked(p, where, device)
+    b, rows = p.batch, k.shape[1]
+    shape = (b, rows, p.heads_kv, p.head_dim)
+    kp = _dense(where, "k", k, torch.bfloat16, shape, device)
+    vp = _dense(where, "v", v, torch.bfloat16, shape, device)
+    cp = _dense(where, "counts", counts, i32, (b,), device)
+    sp = _dense(where, "start", start, i32, (b,), device)
+    _on_device(where, device)
+    _check(lib().dartree_cache_read(ctypes.byref(p), ctypes.byref(cc), rows, kp, vp, cp, sp, st), "dartree_cache_read")
 
 
 def tree_attention_paged_workspace_size(a: AttnParams, p: CacheParams) -> int:
@@ -715,44 +727,25 @@ def tree_attention_paged(a: AttnParams, p: CacheParams, cache: DeviceCache, q, k
     """q [b][B][heads_q][128], k_tree, v_tree [b][B][heads_kv][128] bfloat16 (rows
     of a wider tensor are taken as they are), mask int64 [b][B][ceil(B/64)]
     (None: a chain), out bfloat16 [b][B][heads_q][128]."""
-    where = "tree_attention_paged"
-    cache.check(p, where)
-    _want(where, q_rows=q, k_rows=k_tree, v_rows=v_tree, mask=mask, ctx_len=ctx_len, num_nodes=num_nodes, out=out, ws=ws)
-    _bf16(where, q=q, k_tree=k_tree, v_tree=v_tree, out=out)
-    _int32(where, ctx_len=ctx_len, num_nodes=num_nodes)
-    b, n = a.batch, a.budget
-    for name, t, heads in (("q", q, a.heads_q), ("k_tree", k_tree, a.heads_kv), ("v_tree", v_tree, a.heads_kv),
-                           ("out", out, a.heads_q)):
-        _shape(where, name, t, (b, n, heads, a.head_dim))
-    _want(where, out=out)
-    if mask is not None:
-        _shape(where, "mask", mask, (b, n, (n + 63) // 64))
-        if mask.element_size() != 8:
-            raise ValueError(f"{where}: mask is {mask.dtype}")
-    _shape(where, "ctx_len", ctx_len, (b,))
-    _shape(where, "num_nodes", num_nodes, (b,))
-    stride = _row_stride(where, "k_tree", k_tree)
-    if _row_stride(where, "v_tree", v_tree) != stride:
+    import torch
+    where, bf = "tree_attention_paged", torch.bfloat16
+    device, st = _place(stream)
+    cc = cache.checked(p, where, device)
+    b, n, d = a.batch, a.budget, a.head_dim
+    kv = (b, n, a.heads_kv, d)
+    qp, qstep = _rows(where, "q", q, (bf,), (b, n, a.heads_q, d), device)
+    kp, step = _rows(where, "k_tree", k_tree, (bf,), kv, device)
+    vp, vstep = _rows(where, "v_tree", v_tree, (bf,), kv, device)
+    if step != vstep:
         raise ValueError(f"{where}: the rows of k_tree and v_tree are not equally far apart")
-    cc = cache.c()
-    _check(lib().dartree_tree_attention_paged(ctypes.byref(a), ctypes.byref(p), ctypes.byref(cc), _ptr(q),
-                                              _row_stride(where, "q", q), _ptr(k_tree), _ptr(v_tree), stride, _ptr(mask),
-                                              _ptr(num_nodes), _ptr(ctx_len), _ptr(out), _ptr(ws),
-                                              0 if ws is None else ws.numel() * ws.element_size(), _stream(stream)),
-           "dartree_tree_attention_paged")
-
-
-def _logits(where: str, name: str, t, shape: tuple) -> tuple:
-    """(logits type, elements between rows) of [b][rows][vocab] logits whose rows may be apart."""
-    kind = {"torch.float32": FP32, "torch.bfloat16": BF16}.get(str(t.dtype))
-    if kind is None:
-        raise ValueError(f"{where}: {name} is {t.dtype}")
-    _shape(where, name, t, shape)
-    b, rows, vocab = shape
-    st = t.stride()
-    if (vocab > 1 and st[2] != 1) or (b > 1 and rows > 1 and st[0] != rows * st[1]):
-        raise ValueError(f"{where}: {name} is neither dense nor rows of a wider tensor")
-    return kind, st[1] if rows > 1 else st[0] if b > 1 else vocab
+    op = _dense(where, "out", out, bf, (b, n, a.heads_q, d), device)
+    mp = _dense(where, "mask", mask, torch.int64, (b, n, (n + 63) // 64), device)
+    lp = _dense(where, "ctx_len", ctx_len, torch.int32, (b,), device)
+    np_ = _dense(where, "num_nodes", num_nodes, torch.int32, (b,), device)
+    wp, nbytes = _workspace(where, ws, device)
+    _on_device(where, device)
+    _check(lib().dartree_tree_attention_paged(ctypes.byref(a), ctypes.byref(p), ctypes.byref(cc), qp, qstep, kp, vp, step,
+                                              mp, np_, lp, op, wp, nbytes, st), "dartree_tree_attention_paged")
 
 
 def verify_tree_workspace_size(batch: int, budget: int, max_len: int, vocab: int) -> int:
@@ -774,51 +767,47 @@ def verify_tree(tokens, parents, num_nodes, target_logits, temperature: float, u
     """tokens, parents [b][B] and num_nodes [b] of emitted trees, target_logits
     [b][B+1][V] float32 or bfloat16, uniforms float32 [b][B+1]; outputs accepted
     [b][max_len], num_accepted [b], bonus [b] (int32)."""
-    where = "verify_tree"
+    import torch
+    where, i32 = "verify_tree", torch.int32
+    device, st = _place(stream)
     b, n = tokens.shape
-    vocab, max_len = target_logits.shape[-1], accepted.shape[1]
-    _want(where, tokens=tokens, parents=parents, num_nodes=num_nodes, logits_rows=target_logits, uniforms=uniforms,
-          accepted=accepted, num_accepted=num_accepted, bonus=bonus, ws=ws)
-    _int32(where, tokens=tokens, parents=parents, num_nodes=num_nodes, accepted=accepted, num_accepted=num_accepted,
-           bonus=bonus)
-    kind, stride = _logits(where, "target_logits", target_logits, (b, n + 1, vocab))
-    _shape(where, "parents", parents, (b, n))
-    _shape(where, "uniforms", uniforms, (b, n + 1))
-    _shape(where, "accepted", accepted, (b, max_len))
-    for name, t in (("num_nodes", num_nodes), ("num_accepted", num_accepted), ("bonus", bonus)):
-        _shape(where, name, t, (b,))
-    if str(uniforms.dtype) != "torch.float32":
-        raise ValueError(f"{where}: uniforms is {uniforms.dtype}")
-    _check(lib().dartree_verify_tree(b, n, max_len, vocab, kind, _ptr(tokens), _ptr(parents), _ptr(num_nodes),
-                                     _ptr(target_logits), stride, temperature, _ptr(uniforms), _ptr(accepted),
-                                     _ptr(num_accepted), _ptr(bonus), _ptr(ws),
-                                     0 if ws is None else ws.numel() * ws.element_size(), _stream(stream)),
-           "dartree_verify_tree")
+    vocab, max_len = target_logits.shape[-1], accepted.shape[-1]
+    tp = _dense(where, "tokens", tokens, i32, (b, n), device)
+    pp = _dense(where, "parents", parents, i32, (b, n), device)
+    np_ = _dense(where, "num_nodes", num_nodes, i32, (b,), device)
+    zp, step = _rows(where, "target_logits", target_logits, (torch.float32, torch.bfloat16), (b, n + 1, vocab), device)
+    up = _dense(where, "uniforms", uniforms, torch.float32, (b, n + 1), device)
+    ap = _dense(where, "accepted", accepted, i32, (b, max_len), device)
+    cp = _dense(where, "num_accepted", num_accepted, i32, (b,), device)
+    bp = _dense(where, "bonus", bonus, i32, (b,), device)
+    wp, nbytes = _workspace(where, ws, device)
+    _on_device(where, device)
+    _check(lib().dartree_verify_tree(b, n, max_len, vocab, FP32 if target_logits.dtype is torch.float32 else BF16, tp, pp,
+                                     np_, zp, step, temperature, up, ap, cp, bp, wp, nbytes, st), "dartree_verify_tree")
 
 
 def verify_chain(tokens, target_logits, draft_logits, temperature: float, uniforms, num_accepted, bonus, ws,
                  num_tokens=None, stream=None) -> None:
-    """tokens [b][depth] drawn from draft_logits [b][depth][V], target_logits
-    [b][depth+1][V] (both float32 or both bfloat16), uniforms float32
-    [b][depth+1]; outputs num_accepted [b], bonus [b] (int32)."""
-    where = "verify_chain"
+    """tokens [b][depth] drawn from draft_logits [b][depth][V] (None at
+    temperature 0), target_logits [b][depth+1][V] (both float32 or both
+    bfloat16), uniforms float32 [b][depth+1]; outputs num_accepted [b], bonus [b]."""
+    import torch
+    where, i32 = "verify_chain", torch.int32
+    device, st = _place(stream)
     b, n = tokens.shape
     vocab = target_logits.shape[-1]
-    _want(where, tokens=tokens, num_tokens=num_tokens, target_rows=target_logits, draft_rows=draft_logits,
-          uniforms=uniforms, num_accepted=num_accepted, bonus=bonus, ws=ws)
-    _int32(where, tokens=tokens, num_tokens=num_tokens, num_accepted=num_accepted, bonus=bonus)
-    kind, stride = _logits(where, "target_logits", target_logits, (b, n + 1, vocab))
+    tp = _dense(where, "tokens", tokens, i32, (b, n), device)
+    np_ = _dense(where, "num_tokens", num_tokens, i32, (b,), device)
+    zp, step = _rows(where, "target_logits", target_logits, (torch.float32, torch.bfloat16), (b, n + 1, vocab), device)
+    dp = None
     if draft_logits is not None:
-        # a single draft row has no distance to the next one
-        dkind, dstride = _logits(where, "draft_logits", draft_logits, (b, n, vocab))
-        if dkind != kind or (dstride != stride and b * n > 1):
-            raise ValueError(f"{where}: draft_logits and target_logits differ in type or in the distance of their rows")
-    _shape(where, "uniforms", uniforms, (b, n + 1))
-    for name, t in (("num_tokens", num_tokens), ("num_accepted", num_accepted), ("bonus", bonus)):
-        _shape(where, name, t, (b,))
-    if str(uniforms.dtype) != "torch.float32":
-        raise ValueError(f"{where}: uniforms is {uniforms.dtype}")
-    _check(lib().dartree_verify_chain(b, n, vocab, kind, _ptr(tokens), _ptr(num_tokens), _ptr(target_logits),
-                                      _ptr(draft_logits), stride, temperature, _ptr(uniforms), _ptr(num_accepted),
-                                      _ptr(bonus), _ptr(ws), 0 if ws is None else ws.numel() * ws.element_size(),
-                                      _stream(stream)), "dartree_verify_chain")
+        dp, dstep = _rows(where, "draft_logits", draft_logits, (target_logits.dtype,), (b, n, vocab), device)
+        if dstep != step and b * n > 1:   # a single row has no distance to the next
+            raise ValueError(f"{where}: the rows of draft_logits and target_logits are not equally far apart")
+    up = _dense(where, "uniforms", uniforms, torch.float32, (b, n + 1), device)
+    cp = _dense(where, "num_accepted", num_accepted, i32, (b,), device)
+    bp = _dense(where, "bonus", bonus, i32, (b,), device)
+    wp, nbytes = _workspace(where, ws, device)
+    _on_device(where, device)
+    _check(lib().dartree_verify_chain(b, n, vocab, FP32 if target_logits.dtype is torch.float32 else BF16, tp, np_, zp, dp,
+                                      step, temperature, up, cp, bp, wp, nbytes, st), "dartree_verify_chain")

@@ -130,7 +130,7 @@ def test_verification_refuses_before_any_launch():
 
 def test_binding_names_what_does_not_fit(monkeypatch):
     """Shapes, types and strides that the C call cannot see."""
-    monkeypatch.setattr(torch.cuda, "is_available", lambda: False)   # no device is current: host tensors pass that check
+    monkeypatch.setattr(torch.cuda, "is_initialized", lambda: False)   # before the GPU has been used
     p = D.CacheParams(2, 4, 128, 16, 8, 3, D.CACHE_E4M3)
     c = D.DeviceCache.alloc(p, device="cpu")
     x = torch.zeros(2, 5, 4, 128, dtype=torch.bfloat16)
@@ -150,7 +150,7 @@ def test_binding_names_what_does_not_fit(monkeypatch):
     with pytest.raises(ValueError, match="cache k"):
         D.cache_read(p, D.DeviceCache(c.k.float(), c.v, c.k_exp, c.v_exp, c.table), x, x)
     with pytest.raises(ValueError, match="contiguous"):
-        D.cache_read(p, c, x[:, :, :2].expand(2, 5, 2, 128), x)
+        D.cache_read(p, c, x[:, :, :1].expand(2, 5, 4, 128), x)
     a = D.AttnParams(2, 5, 48, 8, 4, 128, 0.1)
     q = torch.zeros(2, 5, 8, 128, dtype=torch.bfloat16)
     with pytest.raises(ValueError, match="mask"):
@@ -163,8 +163,17 @@ def test_binding_names_what_does_not_fit(monkeypatch):
         D.verify_tree(tok, tok, one, z[:, :5], 1.0, u, acc, one, one, None)
     with pytest.raises(ValueError, match="uniforms"):
         D.verify_tree(tok, tok, one, z, 1.0, u.double(), acc, one, one, None)
-    with pytest.raises(ValueError, match="differ"):
+    with pytest.raises(ValueError, match="draft_logits"):
         D.verify_chain(tok, z, z[:, :5].bfloat16(), 1.0, u, one, one, None)
+    with pytest.raises(ValueError, match="equally far"):
+        D.verify_chain(tok, z, torch.zeros(2, 5, 12)[:, :, :10], 1.0, u, one, one, None)
+    # whatever fits is refused in the end: these tensors are the host's
+    for call in (lambda: D.cache_write(p, c, x, x, 5), lambda: D.cache_read(p, c, x, x),
+                 lambda: D.tree_attention_paged(a, p, c, q, x, x, None, None, q, None),
+                 lambda: D.verify_tree(tok, tok, one, z, 1.0, u, acc, one, one, None),
+                 lambda: D.verify_chain(tok, z, None, 0.0, u, one, one, None)):
+        with pytest.raises(ValueError, match="not on a GPU"):
+            call()
 
 
 def test_plain_quantiser_is_e4m3():
