@@ -7,13 +7,14 @@
 // Exponentials and sums are taken in 64 bits: the final token is where the
 // cumulated mass passes u of the whole, and with 32 bits (1e-7) one draw in
 // sixty of a flat 151936-token row would land on a neighbour.  The vector units
-// do 64-bit fused multiply-adds at the 32-bit rate, so exp64's 20 operations an
-// element stay under the time its bytes take.
+// do 64-bit fused multiply-adds at the 32-bit rate, and ExpTable needs eleven of
+// them an element, so a pass stays near the time its bytes take.
 //
 // Trees: with few rows the records of every row are taken at once (one pass
 // over the logits, all compute units) and a block per request then walks the
 // tree in LDS.  With many, only the rows on the path are read, one level per
-// launch.  Chains: the records of every row, then one pass over the final row.
+// launch, whose last block of a request takes the step.  Chains: the records of
+// every row, then one pass over the final row.
 #include <algorithm>
 
 #include "reduce.hpp"
@@ -33,6 +34,37 @@ struct Record {
   int32_t arg;  // its first index
   double s;     // sum of exp((z - m) / T)
 };
+
+// What blocks of one launch hand to the request's last block goes past the
+// caches of a compute unit and an XCD (relaxed atomics of the device's scope), and
+// a block arrives once its words are there.  A release and an acquire instead
+// write back and drop a whole L2: 24 us for the final token of eight chains
+// against 17.
+__device__ __forceinline__ void hand_over(uint64_t* p, uint64_t x) {
+  __hip_atomic_store(p, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ uint64_t taken_over(const uint64_t* p) {
+  return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ bool arrive_last(int32_t* arrived, int blocks) {
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  return __hip_atomic_fetch_add(arrived, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == blocks - 1;
+}
+
+struct RecordWords {
+  uint64_t w[2];
+};
+__device__ __forceinline__ void put_record(Record* to, const Record& r) {
+  const RecordWords x = __builtin_bit_cast(RecordWords, r);
+  hand_over(reinterpret_cast<uint64_t*>(to), x.w[0]);
+  hand_over(reinterpret_cast<uint64_t*>(to) + 1, x.w[1]);
+}
+template <bool TAKEN>   // TAKEN: written in this launch
+__device__ __forceinline__ Record get_record(const Record* from) {
+  if (!TAKEN) return *from;
+  const uint64_t* p = reinterpret_cast<const uint64_t*>(from);
+  return __builtin_bit_cast(Record, RecordWords{{taken_over(p), taken_over(p + 1)}});
+}
 
 // exp(x) for x <= 0 (or -inf): 2^n 2^f with |f| <= 1/2, the Taylor series of
 // 2^f to degree 12 (the next term is below 2e-16).  x is given times log2(e).
@@ -55,6 +87,41 @@ __device__ __forceinline__ double exp64(double t) {
   return __builtin_ldexp(p, int(n));
 }
 
+// 2^(i / 32)
+__constant__ double kExp32[32] = {
+    1.0, 1.0218971486541166, 1.0442737824274138, 1.0671404006768237,
+    1.0905077326652577, 1.1143867425958924, 1.1387886347566916, 1.1637248587775775,
+    1.189207115002721, 1.215247359980469, 1.241857812073484, 1.2690509571917332,
+    1.2968395546510096, 1.3252366431597413, 1.3542555469368927, 1.383909881963832,
+    1.4142135623730951, 1.4451808069770467, 1.4768261459394993, 1.5091644275934228,
+    1.5422108254079407, 1.5759808451078865, 1.6104903319492543, 1.645755478153965,
+    1.681792830507429, 1.718619298122478, 1.7562521603732995, 1.7947090750031072,
+    1.8340080864093424, 1.8741676341103, 1.9152065613971474, 1.9571441241754002,
+};
+
+// The same for the many elements of a pass: exp((z - m) / T) = 2^(n / 32) 2^(f / 32),
+// |f| <= 1/2, from a table in LDS (32 entries take 64 banks: no conflicts) and a
+// series to degree 4 (the next term is below 2e-12).  NaN and -inf give 2^-1000,
+// nothing beside a sum that is at least 1; z above m gives 1.
+struct ExpTable {
+  const double* table;   // LDS
+  double c32, mc32;      // 32 log2(e) / T, m times that
+  __device__ ExpTable(const double* t, double c, float m) : table(t), c32(32.0 * c), mc32(double(m) * (32.0 * c)) {}
+  __device__ void add(float z, double& sum) const {
+    constexpr double kRound = 6755399441055744.0;   // 1.5 * 2^52: adding it leaves the nearest whole number in the low bits
+    const double t = fmin(fmax(fma(double(z), c32, -mc32), -32000.0), 0.0);
+    const double r = t + kRound, f = t - (r - kRound);
+    const int n = int(uint32_t(__builtin_bit_cast(uint64_t, r)));
+    double p = 9.172562701824643e-09;
+    p = fma(p, f, 1.6938509724371819e-06);
+    p = fma(p, f, 0.00023459619820224677);
+    p = fma(p, f, 0.02166084939249829);
+    p = fma(p, f, 1.0);
+    const uint64_t e = __builtin_bit_cast(uint64_t, table[n & 31]) + (uint64_t(uint32_t(n & ~31) << 15) << 32);
+    sum = fma(__builtin_bit_cast(double, e), p, sum);
+  }
+};
+
 __device__ __forceinline__ float sane(float z) { return z != z ? -INFINITY : fminf(z, 3.40282347e+38f); }
 
 // Row of logits as 16-byte chunks counted from the aligned address at or below
@@ -71,14 +138,18 @@ struct RowView {
   __device__ float at(int i) const {
     return sane(BF ? bf16_to_f32(reinterpret_cast<const uint16_t*>(base)[i]) : reinterpret_cast<const float*>(base)[i]);
   }
-  // elements of chunk c (first: the index of its first); -inf where there is none
+  // elements of chunk c (first: the index of its first); -inf where there is
+  // none.  RAW: NaN and +inf as they are
+  template <bool RAW = false>
   __device__ void load(int c, float (&x)[N], int& first) const {
     first = c * N - shift;
     if (first >= 0 && first + N <= vocab) {
       const u32x4 w = *reinterpret_cast<const u32x4*>(base + int64_t(first) * (BF ? 2 : 4));
 #pragma unroll
-      for (int i = 0; i < N; ++i)
-        x[i] = sane(BF ? __uint_as_float((i & 1) ? w[i >> 1] & 0xFFFF0000u : w[i >> 1] << 16) : __uint_as_float(w[BF ? 0 : i]));
+      for (int i = 0; i < N; ++i) {
+        x[i] = BF ? __uint_as_float((i & 1) ? w[i >> 1] & 0xFFFF0000u : w[i >> 1] << 16) : __uint_as_float(w[BF ? 0 : i]);
+        if (!RAW) x[i] = sane(x[i]);
+      }
     } else {
 #pragma unroll
       for (int i = 0; i < N; ++i) x[i] = first + i >= 0 && first + i < vocab ? at(first + i) : -INFINITY;
@@ -98,27 +169,40 @@ __device__ __forceinline__ int wave_min_int(int x) {
 }
 __device__ __forceinline__ int wave_max_int(int x) { return -wave_min_int(-x); }
 
-// Record of segment `seg` of a row, by a block of 256 threads.
-template <bool BF>
-__device__ __forceinline__ void segment_record(const RowView<BF>& z, int seg, double c, Record* out) {
-  constexpr int N = RowView<BF>::N, L = kSeg / N / 256;
-  __shared__ float sm[4];
-  __shared__ int sa[4];
-  __shared__ double ss[4];
+// A block's share of a segment in registers, and the segment's record from it.
+template <bool BF, int NT>
+struct Segment {
+  static constexpr int N = RowView<BF>::N, L = kSeg / N / NT;
   float x[L][N];
   int first[L];
-  float m = -INFINITY;
+  __device__ Segment(const RowView<BF>& z, int seg) {
 #pragma unroll
-  for (int l = 0; l < L; ++l) z.load(seg * (kSeg / N) + l * 256 + threadIdx.x, x[l], first[l]);
+    for (int l = 0; l < L; ++l) z.template load<true>(seg * (kSeg / N) + l * NT + threadIdx.x, x[l], first[l]);
+  }
+};
+template <bool BF, int NT>
+__device__ __forceinline__ void segment_record(const Segment<BF, NT>& in, double c, Record* out) {
+  constexpr int N = RowView<BF>::N, L = kSeg / N / NT, W = NT / 64;
+  __shared__ double table[32];
+  __shared__ float sm[W];
+  __shared__ int sa[W];
+  __shared__ double ss[W];
+  const auto& x = in.x;
+  const auto& first = in.first;
+  float m = -INFINITY;
+  if (threadIdx.x < 32) table[threadIdx.x] = kExp32[threadIdx.x];
 #pragma unroll
   for (int l = 0; l < L; ++l)
 #pragma unroll
-    for (int i = 0; i < N; ++i) m = fmaxf(m, x[l][i]);
+    for (int i = 0; i < N; ++i) m = fmaxf(m, x[l][i]);   // passes over NaN
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   m = wave_max(m);
   if (lane == 0) sm[wave] = m;
   __syncthreads();
-  m = fmaxf(fmaxf(sm[0], sm[1]), fmaxf(sm[2], sm[3]));
+  m = sm[0];
+#pragma unroll
+  for (int w = 1; w < W; ++w) m = fmaxf(m, sm[w]);
+  m = fminf(m, 3.40282347e+38f);
   int arg = INT32_MAX;
   double s = 0.0;
   if (m != -INFINITY) {
@@ -127,13 +211,13 @@ __device__ __forceinline__ void segment_record(const RowView<BF>& z, int seg, do
       for (int l = 0; l < L; ++l)
 #pragma unroll
         for (int i = 0; i < N; ++i)
-          if (x[l][i] == m) arg = min(arg, first[l] + i);
+          if (x[l][i] >= m) arg = min(arg, first[l] + i);
     } else {
-      const double md = m;
+      const ExpTable e(table, c, m);
 #pragma unroll
       for (int l = 0; l < L; ++l)
 #pragma unroll
-        for (int i = 0; i < N; ++i) s += exp64((double(x[l][i]) - md) * c);
+        for (int i = 0; i < N; ++i) e.add(x[l][i], s);
     }
   }
   if (c == 0.0) {
@@ -147,39 +231,57 @@ __device__ __forceinline__ void segment_record(const RowView<BF>& z, int seg, do
   if (threadIdx.x == 0) {
     Record r;
     r.m = m;
-    r.arg = c == 0.0 ? min(min(sa[0], sa[1]), min(sa[2], sa[3])) : 0;
-    r.s = c == 0.0 ? 0.0 : (ss[0] + ss[1]) + (ss[2] + ss[3]);
-    *out = r;
+    r.arg = c == 0.0 ? sa[0] : 0;
+    r.s = c == 0.0 ? 0.0 : ss[0];
+#pragma unroll
+    for (int w = 1; w < W; ++w) {
+      if (c == 0.0) r.arg = min(r.arg, sa[w]);
+      else r.s += ss[w];
+    }
+    put_record(out, r);
   }
 }
 
-// A row's records joined by 16 lanes (all 64 of a wave must call); the same in each.
+// A row's records joined by 8 lanes (kJoin); the same in each.
+constexpr int kJoin = 8;
+template <bool TAKEN = false>
 __device__ __forceinline__ Record join_records(const Record* rec, int nseg, double c) {
-  const int l16 = threadIdx.x & 15;
+  constexpr int H = 5;   // records at a time: 8 x 5 are those of 163840 tokens
+  const int l = threadIdx.x & (kJoin - 1);
   Record r{-INFINITY, INT32_MAX, 0.0};
-  for (int i = l16; i < nseg; i += 16) {   // indices grow, so an equal maximum keeps the first
-    const Record o = rec[i];
-    if (o.m == -INFINITY) continue;
-    if (o.m > r.m) {
-      r.s = r.m == -INFINITY ? o.s : r.s * exp64((double(r.m) - double(o.m)) * c) + o.s;
-      r.m = o.m;
-      r.arg = o.arg;
-    } else {
-      r.s += o.s * exp64((double(o.m) - double(r.m)) * c);
-    }
-  }
+  for (int i0 = l; i0 < nseg; i0 += kJoin * H) {
+    Record o[H];
+    float m = r.m;
 #pragma unroll
-  for (int off = 1; off < 16; off <<= 1) {
-    const float m = __shfl_xor(r.m, off);
-    const int arg = __shfl_xor(r.arg, off);
-    const double s = __shfl_xor(r.s, off);
-    const float top = fmaxf(r.m, m);
-    // the same expression on both sides, so that all lanes agree to the bit
-    const double mine = r.m == -INFINITY ? 0.0 : r.s * exp64((double(r.m) - double(top)) * c);
-    const double theirs = m == -INFINITY ? 0.0 : s * exp64((double(m) - double(top)) * c);
-    r.arg = r.m == m ? min(r.arg, arg) : r.m > m ? r.arg : arg;
-    r.s = mine + theirs;
-    r.m = top;
+    for (int h = 0; h < H; ++h) {
+      o[h] = get_record<TAKEN>(rec + min(i0 + kJoin * h, nseg - 1));
+      if (i0 + kJoin * h >= nseg) o[h].m = -INFINITY;
+      m = fmaxf(m, o[h].m);
+    }
+    if (m == -INFINITY) continue;
+    if (m > r.m) {
+      r.s = r.m == -INFINITY ? 0.0 : r.s * exp64((double(r.m) - double(m)) * c);
+      r.arg = INT32_MAX;
+      r.m = m;
+    }
+#pragma unroll
+    for (int h = 0; h < H; ++h)
+      if (o[h].m != -INFINITY) {
+        if (o[h].m == m) r.arg = min(r.arg, o[h].arg);
+        r.s += o[h].s * exp64((double(o[h].m) - double(m)) * c);
+      }
+  }
+  float m = r.m;
+#pragma unroll
+  for (int off = 1; off < kJoin; off <<= 1) m = fmaxf(m, __shfl_xor(m, off));
+  if (m == -INFINITY) return r;
+  if (r.m != m) r.arg = INT32_MAX;
+  r.s = r.m == -INFINITY ? 0.0 : r.s * exp64((double(r.m) - double(m)) * c);
+  r.m = m;
+#pragma unroll
+  for (int off = 1; off < kJoin; off <<= 1) {   // a sum of the same two numbers on both sides
+    r.arg = min(r.arg, __shfl_xor(r.arg, off));
+    r.s += __shfl_xor(r.s, off);
   }
   return r;
 }
@@ -196,29 +298,34 @@ struct Law {
   __device__ double share(float z, int i) const { return empty() ? 0.0 : c == 0.0 ? weight(z, i) : weight(z, i) / s; }
 };
 
-// Threads of a block (blockDim.x a multiple of 64, at most 1024) that agree on
-// the first token whose cumulated weight passes `target` in segment `seg`, where
-// `weight(c, w)` gives the weights of chunk c (w[i] of element first + i, 0
-// where there is none) and returns first.  -1 if none does and, in *last, the
-// last token of positive weight (-1: none).
-template <int N, typename F>
+// The first token whose cumulated weight passes `target` in segment `seg`,
+// by a block of NT threads; `weight(c, w)` gives the weights of chunk c (w[i] of
+// element first + i, 0 where there is none) and returns first.  -1 if none does
+// and, in *last, the segment's last token of positive weight (-1: none).
+template <int NT, int N, typename F>
 __device__ __forceinline__ int pick_in_segment(int seg, double target, F&& weight, int* last) {
-  __shared__ double wsum[16];
+  constexpr int kChunks = kSeg / N, kEach = kChunks > NT ? kChunks / NT : 1;   // consecutive chunks per thread
+  __shared__ double wsum[NT / 64];
   __shared__ int got[2];
-  const int nt = blockDim.x, waves = nt >> 6, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int chunks = kSeg / N, each = (chunks + nt - 1) / nt;   // consecutive chunks per thread
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   if (threadIdx.x == 0) {
     got[0] = INT32_MAX;
     got[1] = -1;
   }
-  double sum = 0.0;
-  for (int k = 0; k < each; ++k) {
-    const int c = int(threadIdx.x) * each + k;
-    if (c >= chunks) break;
-    double w[N];
-    weight(seg * chunks + c, w);
+  double w[kEach][N], sum = 0.0;
+  int first[kEach];
 #pragma unroll
-    for (int i = 0; i < N; ++i) sum += w[i];
+  for (int k = 0; k < kEach; ++k) {
+    const int c = int(threadIdx.x) * kEach + k;
+    first[k] = 0;
+    if (c < kChunks) {
+      first[k] = weight(seg * kChunks + c, w[k]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) w[k][i] = 0.0;
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) sum += w[k][i];
   }
   double incl = sum;
 #pragma unroll
@@ -229,21 +336,16 @@ __device__ __forceinline__ int pick_in_segment(int seg, double target, F&& weigh
   if (lane == 63) wsum[wave] = incl;
   __syncthreads();
   double cum = incl - sum;
-  for (int w = 0; w < wave && w < waves; ++w) cum += wsum[w];
+  for (int x = 0; x < wave; ++x) cum += wsum[x];
   int found = INT32_MAX, pos = -1;
-  if (sum > 0.0)
-    for (int k = 0; k < each; ++k) {
-      const int c = int(threadIdx.x) * each + k;
-      if (c >= chunks) break;
-      double w[N];
-      const int first = weight(seg * chunks + c, w);
 #pragma unroll
-      for (int i = 0; i < N; ++i) {
-        cum += w[i];
-        if (w[i] > 0.0) {
-          pos = first + i;
-          if (found == INT32_MAX && cum > target) found = first + i;
-        }
+  for (int k = 0; k < kEach; ++k)
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      cum += w[k][i];
+      if (w[k][i] > 0.0) {
+        pos = first[k] + i;
+        if (found == INT32_MAX && cum > target) found = pos;
       }
     }
   found = wave_min_int(found);
@@ -260,11 +362,11 @@ __device__ __forceinline__ int pick_in_segment(int seg, double target, F&& weigh
 }
 
 // The weight of a segment, in every thread of the block.
-template <int N, typename F>
+template <int NT, int N, typename F>
 __device__ __forceinline__ double segment_weight(int seg, F&& weight) {
-  __shared__ double wsum[16];
+  __shared__ double wsum[NT / 64];
   double sum = 0.0;
-  for (int c = threadIdx.x; c < kSeg / N; c += blockDim.x) {
+  for (int c = threadIdx.x; c < kSeg / N; c += NT) {
     double w[N];
     weight(seg * (kSeg / N) + c, w);
 #pragma unroll
@@ -275,13 +377,13 @@ __device__ __forceinline__ double segment_weight(int seg, F&& weight) {
   if ((threadIdx.x & 63) == 0) wsum[threadIdx.x >> 6] = sum;
   __syncthreads();
   sum = 0.0;
-  for (int w = 0; w < int(blockDim.x >> 6); ++w) sum += wsum[w];
+  for (int w = 0; w < NT / 64; ++w) sum += wsum[w];
   return sum;
 }
 
 // The first token whose cumulated weight passes u of the whole, given the
 // segments' weights in LDS (block-uniform result; -1: no weight at all).
-template <int N, typename F>
+template <int NT, int N, typename F>
 __device__ __forceinline__ int pick(const double* seg_weight, int nseg, float u, F&& weight) {
   __shared__ double target;
   __shared__ int chosen;
@@ -318,13 +420,13 @@ __device__ __forceinline__ int pick(const double* seg_weight, int nseg, float u,
   const int sg = chosen;
   int last = -1;
   if (sg >= 0) {
-    const int got = pick_in_segment<N>(sg, target, weight, &last);
+    const int got = pick_in_segment<NT, N>(sg, target, weight, &last);
     if (got >= 0) return got;
     if (last >= 0) return last;   // a sum rounded differently: the segment's last token
   }
   // u at or past 1 (or not a number): the row's last token of positive weight
   for (int s = nseg - 1; s >= 0 && last < 0; --s) {
-    const int got = pick_in_segment<N>(s, INFINITY, weight, &last);
+    const int got = pick_in_segment<NT, N>(s, INFINITY, weight, &last);
     if (got >= 0) return got;
   }
   return last;
@@ -334,54 +436,48 @@ __device__ __forceinline__ int pick(const double* seg_weight, int nseg, float u,
 // Records
 // ---------------------------------------------------------------------------
 
-// Every row: block (row, segment).
+// Every row of z, then those of y: block (row, segment).
 template <bool BF>
-__global__ __launch_bounds__(256) void row_records(const void* z, int64_t stride, int vocab, int nseg, double c, Record* rec) {
+__global__ __launch_bounds__(256) void row_records(const void* z, int64_t zrows, const void* y, int64_t stride, int vocab, int nseg,
+                                                   double c, Record* rec, int32_t* counters, int ncounters) {
+  if (blockIdx.x == 0)   // for the next launch
+    for (int i = threadIdx.x; i < ncounters; i += 256) counters[i] = 0;
   const int row = blockIdx.x / nseg, seg = blockIdx.x - row * nseg;
-  const RowView<BF> v(z, row, stride, vocab);
-  segment_record<BF>(v, seg, c, rec + blockIdx.x);
-}
-
-// State of a request's walk (level by level).
-struct Walk {
-  int32_t at, count, done, pad;
-};
-
-// The current row of every request: block (request, segment).
-template <bool BF>
-__global__ __launch_bounds__(256) void level_records(VerifyArgs a, int nseg, double c, Walk* walk, Record* rec, int level) {
-  const int q = blockIdx.x / nseg, seg = blockIdx.x - q * nseg;
-  Walk w{-1, 0, 0, 0};
-  if (level > 0) w = walk[q];
-  if (w.done) return;
-  const RowView<BF> v(a.target, int64_t(q) * (a.budget + 1) + w.at + 1, a.row_stride, a.vocab);
-  segment_record<BF>(v, seg, c, rec + blockIdx.x);
+  const RowView<BF> v(row < zrows ? z : y, row < zrows ? row : row - zrows, stride, vocab);
+  segment_record<BF, 256>(Segment<BF, 256>(v, seg), c, rec + blockIdx.x);
 }
 
 // ---------------------------------------------------------------------------
 // Trees
 // ---------------------------------------------------------------------------
 
-// The final token of row `row` without the tokens of `gone` (LDS), by a block.
-template <bool BF>
+// The final token of row `row` without the tokens of `gone` (LDS; the shares of the
+// first kShares in `share`), by a block of NT threads.
+constexpr int kShares = 64;
+template <bool BF, int NT, bool TAKEN>
 __device__ int final_token(const VerifyArgs& a, int64_t row, const Record* rec, int nseg, const Law& law, const int32_t* gone,
-                           int ngone, float u, double* segw) {
+                           const double* share, int ngone, float u, double* segw) {
   constexpr int N = RowView<BF>::N;
   const RowView<BF> z(a.target, row, a.row_stride, a.vocab);
   if (law.empty()) return -1;
   if (law.c == 0.0) return law.arg;   // all of the mass on one token: it remains, or nothing does and p decides
   for (int pass = 0; pass < 2; ++pass) {   // second: nothing was left of p
     const int n = pass == 0 ? ngone : 0;
-    __syncthreads();
-    for (int s = threadIdx.x; s < nseg; s += blockDim.x) {
-      const Record r = rec[s];
+    bool again = false;
+    for (int s = threadIdx.x; s < nseg; s += NT) {
+      const Record r = get_record<TAKEN>(rec + s);
       const double all = r.m == -INFINITY ? 0.0 : r.s * exp64((double(r.m) - law.m) * law.c);
       double w = all;
+      bool many = false;
       for (int i = 0; i < n; ++i) {
-        const int t = gone[i];
-        if ((t + z.shift) / kSeg == s) w -= law.weight(z.at(t), t);
+        if ((gone[i] + z.shift) / kSeg != s) continue;
+        if (i < kShares) w -= share[i] * law.s;
+        else many = true;
       }
-      segw[s] = w == all || w > 1e-4 * all ? w : -1.0;   // -1: little is left of the sum, add it up again
+      // little is left of a sum, or its tokens' shares are not at hand: add it up again
+      const bool redo = many || (w != all && w <= 1e-4 * all);
+      segw[s] = redo ? -1.0 : w;
+      again |= redo;
     }
     auto weight = [&](int chunk, double (&w)[N]) {
       float x[N];
@@ -397,23 +493,24 @@ __device__ int final_token(const VerifyArgs& a, int64_t row, const Record* rec, 
       }
       return first;
     };
-    __syncthreads();
-    for (int s = 0; s < nseg && n > 0; ++s)
-      if (segw[s] < 0.0) {   // the same for all threads
-        const double w = segment_weight<N>(s, weight);
-        if (threadIdx.x == 0) segw[s] = w;
-      }
-    const int t = pick<N>(segw, nseg, u, weight);
+    if (__syncthreads_or(again))
+      for (int s = 0; s < nseg; ++s)
+        if (segw[s] < 0.0) {   // the same for all threads
+          const double w = segment_weight<NT, N>(s, weight);
+          if (threadIdx.x == 0) segw[s] = w;
+        }
+    const int t = pick<NT, N>(segw, nseg, u, weight);
     if (t >= 0) return t;
+    __syncthreads();
   }
   return -1;
 }
 
-constexpr int kWalkNodes = 1024;   // nodes of a tree walked in LDS
+constexpr int kWalkNodes = 1024;   // nodes of a tree walked in LDS, and threads of its block
 
 // All rows' records at hand: a block per request.
 template <bool BF>
-__global__ __launch_bounds__(512) void tree_walk(VerifyArgs a, int nseg, double c, const Record* rec) {
+__global__ __launch_bounds__(kWalkNodes) void tree_walk(VerifyArgs a, int nseg, double c, const Record* rec) {
   __shared__ int32_t tok[kWalkNodes], par[kWalkNodes];
   __shared__ float us[kWalkNodes];
   __shared__ double share[kWalkNodes];
@@ -426,26 +523,29 @@ __global__ __launch_bounds__(512) void tree_walk(VerifyArgs a, int nseg, double 
   const int n = min(max(a.num_nodes[q], 0), B);
   const int lane = threadIdx.x & 63;
   const Record* qrec = rec + int64_t(q) * (B + 1) * nseg;
-  for (int row = threadIdx.x >> 4; row < ((n + 4) & ~3); row += blockDim.x >> 4) {   // whole waves
-    const Record r = join_records(qrec + int64_t(min(row, n)) * nseg, nseg, c);
-    if ((threadIdx.x & 15) == 0 && row <= n) {
+  // the drafted tokens' logits, then the rows' laws, then the tokens' shares
+  const int j = threadIdx.x;
+  float zj = -INFINITY;
+  if (j < n) {
+    const int t = a.tokens[int64_t(q) * B + j], p = a.parents[int64_t(q) * B + j];
+    tok[j] = t;
+    par[j] = p;
+    us[j] = a.uniforms[int64_t(q) * (B + 1) + j + 1];
+    if (p >= -1 && p < n && t >= 0 && t < a.vocab)
+      zj = RowView<BF>(a.target, int64_t(q) * (B + 1) + p + 1, a.row_stride, a.vocab).at(t);
+  }
+  for (int row = threadIdx.x / kJoin; row <= n; row += kWalkNodes / kJoin) {
+    const Record r = join_records(qrec + int64_t(row) * nseg, nseg, c);
+    if (threadIdx.x % kJoin == 0) {
       rm[row] = r.m;
       rarg[row] = r.arg;
       rs[row] = r.s;
     }
   }
   __syncthreads();
-  for (int j = threadIdx.x; j < n; j += blockDim.x) {
-    const int t = a.tokens[int64_t(q) * B + j], p = a.parents[int64_t(q) * B + j];
-    tok[j] = t;
-    par[j] = p;
-    us[j] = a.uniforms[int64_t(q) * (B + 1) + j + 1];
-    double s = 0.0;
-    if (p >= -1 && p < n && t >= 0 && t < a.vocab) {
-      const RowView<BF> z(a.target, int64_t(q) * (B + 1) + p + 1, a.row_stride, a.vocab);
-      s = Law(Record{rm[p + 1], rarg[p + 1], rs[p + 1]}, c).share(z.at(t), t);
-    }
-    share[j] = s;
+  if (j < n) {
+    const int p = par[j], t = tok[j];
+    share[j] = p >= -1 && p < n && t >= 0 && t < a.vocab ? Law(Record{rm[p + 1], rarg[p + 1], rs[p + 1]}, c).share(zj, t) : 0.0;
   }
   __syncthreads();
   if (threadIdx.x < 64) {
@@ -480,13 +580,17 @@ __global__ __launch_bounds__(512) void tree_walk(VerifyArgs a, int nseg, double 
       tested_s = tested;
       a.num_accepted[q] = count;
     }
-    // the tested children's tokens, gathered where the tree's tokens were
+    // the tested children's tokens and shares, gathered where the tree's were
     int m = 0;
     for (int j0 = 0; j0 < n && tested; j0 += 64) {
       const bool kid = j0 + lane < n && par[j0 + lane] == at && tok[j0 + lane] >= 0 && tok[j0 + lane] < a.vocab;
       const int t = kid ? tok[j0 + lane] : 0;
+      const double s = kid ? share[j0 + lane] : 0.0;
       const uint64_t b = __ballot(kid);
-      if (kid) tok[m + __popcll(b & ((1ull << lane) - 1))] = t;
+      if (kid) {
+        tok[m + __popcll(b & ((1ull << lane) - 1))] = t;
+        share[m + __popcll(b & ((1ull << lane) - 1))] = s;
+      }
       m += __popcll(b);
     }
     if (lane == 0) tested_s = m;
@@ -494,29 +598,45 @@ __global__ __launch_bounds__(512) void tree_walk(VerifyArgs a, int nseg, double 
   __syncthreads();
   const int at = at_s;
   const Law law(Record{rm[at + 1], rarg[at + 1], rs[at + 1]}, c);
-  const int t = final_token<BF>(a, int64_t(q) * (B + 1) + at + 1, qrec + int64_t(at + 1) * nseg, nseg, law, tok, tested_s,
+  const int t = final_token<BF, kWalkNodes, false>(a, int64_t(q) * (B + 1) + at + 1, qrec + int64_t(at + 1) * nseg, nseg, law, tok, share, tested_s,
                                 a.uniforms[int64_t(q) * (B + 1)], segw);
   if (threadIdx.x == 0) a.bonus[q] = t;
 }
 
-// One level: the records of the current row at hand, a block per request.
+constexpr int kPick = 512;   // threads of the blocks below
+
+// State of a request's walk, level by level.
+struct Walk {
+  int32_t at, count, done, arrived;   // arrived: blocks of this level whose record is written
+};
+__global__ __launch_bounds__(256) void walk_begin(Walk* walk, int batch) {
+  const int q = blockIdx.x * 256 + threadIdx.x;
+  if (q < batch) walk[q] = Walk{-1, 0, 0, 0};
+}
+
+// One level: block (request, segment) takes the record of its segment of the
+// current row, and the request's last block to arrive takes the step.
 template <bool BF>
-__global__ __launch_bounds__(256) void level_step(VerifyArgs a, int nseg, double c, Walk* walk, const Record* rec, int level) {
-  __shared__ int32_t kid[DARTREE_MAX_SORT], gone[DARTREE_MAX_SORT];
-  __shared__ int wcount[4], next_s, ngone_s;
+__global__ __launch_bounds__(kPick) void walk_level(VerifyArgs a, int nseg, double c, Walk* walk, Record* rec) {
+  __shared__ uint16_t kid[DARTREE_MAX_SORT];
+  __shared__ int32_t gone[DARTREE_MAX_SORT], tkid[kPick];   // tkid, ukid, zkid: the first kPick children
+  __shared__ float ukid[kPick], zkid[kPick];
+  __shared__ double share[kShares];
+  __shared__ int wcount[kPick / 64], next_s, ngone_s, last_s;
   __shared__ double segw[kMaxSeg];
-  const int q = blockIdx.x, B = a.budget, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  Walk w{-1, 0, 0, 0};
-  if (level > 0) w = walk[q];
+  const int q = blockIdx.x / nseg, seg = blockIdx.x - q * nseg, B = a.budget;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const Walk w = walk[q];   // `arrived` changes meanwhile and is not used
   if (w.done) return;
-  const int n = min(max(a.num_nodes[q], 0), B);
   const int64_t row = int64_t(q) * (B + 1) + w.at + 1;
-  const Record r = join_records(rec + int64_t(q) * nseg, nseg, c);
-  const Law law(r, c);
   const RowView<BF> z(a.target, row, a.row_stride, a.vocab);
+  const Segment<BF, kPick> part(z, seg);
+  // the current node's children in index order, in every block while its segment
+  // arrives: the last block needs them at once
+  const int n = min(max(a.num_nodes[q], 0), B);
   int nkid = 0;
   if (w.count < min(a.max_len, n))
-    for (int j0 = 0; j0 < n; j0 += 256) {   // the children in index order
+    for (int j0 = 0; j0 < n; j0 += kPick) {
       const int j = j0 + threadIdx.x;
       const bool is = j < n && a.parents[int64_t(q) * B + j] == w.at;
       const uint64_t b = __ballot(is);
@@ -524,34 +644,51 @@ __global__ __launch_bounds__(256) void level_step(VerifyArgs a, int nseg, double
       if (lane == 0) wcount[wave] = __popcll(b);
       __syncthreads();
       int at = nkid + __popcll(b & ((1ull << lane) - 1));
-      for (int x = 0; x < wave; ++x) at += wcount[x];
-      if (is) kid[at] = j;
-      nkid += wcount[0] + wcount[1] + wcount[2] + wcount[3];
+      for (int x = 0; x < kPick / 64; ++x) {
+        if (x < wave) at += wcount[x];
+        nkid += wcount[x];
+      }
+      if (is) kid[at] = uint16_t(j);
     }
   __syncthreads();
+  auto read_kid = [&](int i, int& t, float& u, float& x) {
+    t = a.tokens[int64_t(q) * B + kid[i]];
+    u = a.uniforms[int64_t(q) * (B + 1) + kid[i] + 1];
+    x = t >= 0 && t < a.vocab ? z.at(t) : -INFINITY;
+  };
+  if (int(threadIdx.x) < nkid) read_kid(threadIdx.x, tkid[threadIdx.x], ukid[threadIdx.x], zkid[threadIdx.x]);
+  segment_record<BF, kPick>(part, c, rec + blockIdx.x);
+  if (threadIdx.x == 0) last_s = arrive_last(&walk[q].arrived, nseg);   // the thread that put the record
+  __syncthreads();
+  if (!last_s) return;
+  const Law law(join_records<true>(rec + int64_t(q) * nseg, nseg, c), c);
   if (wave == 0) {
     double taken = 0.0;
     int next = -1, m = 0;
     for (int i0 = 0; i0 < nkid && next < 0; i0 += 64) {
-      const int j = i0 + lane < nkid ? kid[i0 + lane] : -1;
-      const int t = j >= 0 ? a.tokens[int64_t(q) * B + j] : -1;
+      const int i = i0 + lane;
+      int t = -1;
+      float u = 0.f, x = -INFINITY;
+      if (i < min(nkid, kPick)) t = tkid[i], u = ukid[i], x = zkid[i];
+      else if (i < nkid) read_kid(i, t, u, x);
       const bool in = t >= 0 && t < a.vocab;
-      const double s = in ? law.share(z.at(t), t) : 0.0;
-      const float u = j >= 0 ? a.uniforms[int64_t(q) * (B + 1) + j + 1] : 0.f;
+      const double s = in ? law.share(x, t) : 0.0;
       const uint64_t b = __ballot(in);
-      if (in) gone[m + __popcll(b & ((1ull << lane) - 1))] = t;
+      const int at = m + __popcll(b & ((1ull << lane) - 1));
+      if (in) gone[at] = t;
+      if (in && at < kShares) share[at] = s;
       m += __popcll(b);
-      for (int i = 0; i < min(64, nkid - i0); ++i) {
-        const double si = __shfl(s, i);
-        if (double(__shfl(u, i)) * (1.0 - taken) < si) {
-          next = __shfl(j, i);
+      for (int x0 = 0; x0 < min(64, nkid - i0); ++x0) {
+        const double si = __shfl(s, x0);
+        if (double(__shfl(u, x0)) * (1.0 - taken) < si) {
+          next = i0 + x0;
           break;
         }
         taken += si;
       }
     }
     if (lane == 0) {
-      next_s = next;
+      next_s = next < 0 ? -1 : kid[next];
       ngone_s = m;
     }
   }
@@ -564,8 +701,9 @@ __global__ __launch_bounds__(256) void level_step(VerifyArgs a, int nseg, double
     }
     return;
   }
-  for (int j = w.count + threadIdx.x; j < a.max_len; j += 256) a.accepted[int64_t(q) * a.max_len + j] = -1;
-  const int t = final_token<BF>(a, row, rec + int64_t(q) * nseg, nseg, law, gone, ngone_s, a.uniforms[int64_t(q) * (B + 1)], segw);
+  for (int j = w.count + threadIdx.x; j < a.max_len; j += kPick) a.accepted[int64_t(q) * a.max_len + j] = -1;
+  const int t = final_token<BF, kPick, true>(a, row, rec + int64_t(q) * nseg, nseg, law, gone, share, ngone_s,
+                                a.uniforms[int64_t(q) * (B + 1)], segw);
   if (threadIdx.x == 0) {
     a.num_accepted[q] = w.count;
     a.bonus[q] = t;
@@ -589,12 +727,23 @@ __device__ __forceinline__ int chain_walk(const VerifyArgs& a, int nseg, double 
                                           ChainRows& rows) {
   const int q = blockIdx.y, D = a.budget;
   const int n = a.num_nodes ? min(max(a.num_nodes[q], 0), D) : D;
+  // thread i: token i's logits and random number, while the rows' records arrive
+  const int i = threadIdx.x;
+  int tok = -1;
+  float zt = -INFINITY, yt = -INFINITY, u = 0.f;
+  if (i < n) {
+    tok = a.tokens[int64_t(q) * D + i];
+    if (tok >= 0 && tok < a.vocab) {
+      zt = RowView<BF>(a.target, int64_t(q) * (D + 1) + i, a.row_stride, a.vocab).at(tok);
+      if (c != 0.0) yt = RowView<BF>(a.draft, int64_t(q) * D + i, a.row_stride, a.vocab).at(tok);
+    }
+    u = a.uniforms[int64_t(q) * (D + 1) + i + 1];
+  }
   const int nrow = c == 0.0 ? n + 1 : 2 * n + 1;   // target rows 0 .. n, then the draft's 0 .. n - 1
-  for (int row = threadIdx.x >> 4; row < ((nrow + 3) & ~3); row += blockDim.x >> 4) {   // whole waves
-    const int x = min(row, nrow - 1);
-    const Record* at = x <= n ? trec + (int64_t(q) * (D + 1) + x) * nseg : drec + (int64_t(q) * D + x - n - 1) * nseg;
+  for (int row = threadIdx.x / kJoin; row < nrow; row += kPick / kJoin) {
+    const Record* at = row <= n ? trec + (int64_t(q) * (D + 1) + row) * nseg : drec + (int64_t(q) * D + row - n - 1) * nseg;
     const Record r = join_records(at, nseg, c);
-    if ((threadIdx.x & 15) == 0 && row < nrow) {
+    if (threadIdx.x % kJoin == 0) {
       rows.m[row] = r.m;
       rows.arg[row] = r.arg;
       rows.s[row] = r.s;
@@ -602,23 +751,11 @@ __device__ __forceinline__ int chain_walk(const VerifyArgs& a, int nseg, double 
   }
   __syncthreads();
   if (threadIdx.x < 64) {
-    const int i = threadIdx.x;
     bool pass = false;
-    if (i < n) {
-      const int t = a.tokens[int64_t(q) * D + i];
-      if (t >= 0 && t < a.vocab) {
-        const Law p(Record{rows.m[i], rows.arg[i], rows.s[i]}, c);
-        const RowView<BF> z(a.target, int64_t(q) * (D + 1) + i, a.row_stride, a.vocab);
-        const double px = p.share(z.at(t), t);
-        if (c == 0.0) {
-          pass = px > 0.0;
-        } else {
-          const int d = n + 1 + i;
-          const Law ql(Record{rows.m[d], rows.arg[d], rows.s[d]}, c);
-          const RowView<BF> y(a.draft, int64_t(q) * D + i, a.row_stride, a.vocab);
-          pass = double(a.uniforms[int64_t(q) * (D + 1) + i + 1]) * ql.share(y.at(t), t) < px;
-        }
-      }
+    if (i < n && tok >= 0 && tok < a.vocab) {
+      const double px = Law(Record{rows.m[i], rows.arg[i], rows.s[i]}, c).share(zt, tok);
+      const int d = n + 1 + i;
+      pass = c == 0.0 ? px > 0.0 : double(u) * Law(Record{rows.m[d], rows.arg[d], rows.s[d]}, c).share(yt, tok) < px;
     }
     const uint64_t stop = __ballot(!pass);   // bits at and past n are set, unless n = 64
     if (i == 0) rows.count = stop ? min(__builtin_ctzll(stop), n) : n;
@@ -668,58 +805,45 @@ __device__ __forceinline__ Residual<BF> residual_of(const VerifyArgs& a, double 
                       1.0 / rows.s[k], 1.0 / rows.s[d], reject};
 }
 
-// The residual's weight by segments: block (segment, request).
+// The final token: block (segment, request).  After a rejection every block
+// takes its segment's weight of [p - q]_+ and a request's last block to arrive
+// draws; otherwise the first block draws from p by its records.
 template <bool BF>
-__global__ __launch_bounds__(256) void chain_residual(VerifyArgs a, int nseg, double c, const Record* trec, const Record* drec,
-                                                      double* segw) {
-  constexpr int N = RowView<BF>::N;
-  __shared__ ChainRows rows;
-  __shared__ double ss[4];
-  const int n = chain_walk<BF>(a, nseg, c, trec, drec, rows);
-  const Residual<BF> f = residual_of<BF>(a, c, rows, n);
-  if (!f.reject || f.p.empty()) return;
-  double sum = 0.0;
-  for (int l = 0; l < kSeg / N / 256; ++l) {
-    double w[N];
-    f(blockIdx.x * (kSeg / N) + l * 256 + threadIdx.x, w);
-#pragma unroll
-    for (int i = 0; i < N; ++i) sum += w[i];
-  }
-  sum = wave_sum64(sum);
-  if ((threadIdx.x & 63) == 0) ss[threadIdx.x >> 6] = sum;
-  __syncthreads();
-  if (threadIdx.x == 0) segw[int64_t(blockIdx.y) * nseg + blockIdx.x] = (ss[0] + ss[1]) + (ss[2] + ss[3]);
-}
-
-// The final token: a block per request.
-template <bool BF>
-__global__ __launch_bounds__(256) void chain_final(VerifyArgs a, int nseg, double c, const Record* trec, const Record* drec,
-                                                   const double* segw) {
+__global__ __launch_bounds__(kPick) void chain_final(VerifyArgs a, int nseg, double c, const Record* trec, const Record* drec,
+                                                     uint64_t* segw, int32_t* arrived) {
   constexpr int N = RowView<BF>::N;
   __shared__ ChainRows rows;
   __shared__ double sw[kMaxSeg];
+  __shared__ int last_s;
   const int q = blockIdx.y, D = a.budget;
   const int n = chain_walk<BF>(a, nseg, c, trec, drec, rows);
-  const float u = a.uniforms[int64_t(q) * (D + 1)];
   Residual<BF> f = residual_of<BF>(a, c, rows, n);
   int t = -1;
-  if (f.p.empty()) {
-  } else if (c == 0.0) {
-    t = f.p.arg;
-  } else {
-    if (f.reject) {
-      for (int s = threadIdx.x; s < nseg; s += 256) sw[s] = segw[int64_t(q) * nseg + s];
-      t = pick<N>(sw, nseg, u, f);
+  if (f.reject && !f.p.empty()) {
+    const double sum = segment_weight<kPick, N>(blockIdx.x, f);
+    if (threadIdx.x == 0) {
+      hand_over(segw + int64_t(q) * nseg + blockIdx.x, __builtin_bit_cast(uint64_t, sum));
+      last_s = arrive_last(arrived + q, nseg);
     }
-    if (t < 0) {   // after the last token, or nothing left of p
+    __syncthreads();
+    if (!last_s) return;
+    for (int s = threadIdx.x; s < nseg; s += kPick) sw[s] = __builtin_bit_cast(double, taken_over(segw + int64_t(q) * nseg + s));
+    t = pick<kPick, N>(sw, nseg, a.uniforms[int64_t(q) * (D + 1)], f);
+  } else if (blockIdx.x > 0) {
+    return;
+  }
+  if (t < 0 && !f.p.empty()) {   // after the last token, or nothing left of p
+    if (c == 0.0) {
+      t = f.p.arg;
+    } else {
       f.reject = false;
       const Record* rec = trec + (int64_t(q) * (D + 1) + rows.count) * nseg;
       __syncthreads();
-      for (int s = threadIdx.x; s < nseg; s += 256) {
+      for (int s = threadIdx.x; s < nseg; s += kPick) {
         const Record r = rec[s];
         sw[s] = r.m == -INFINITY ? 0.0 : r.s * exp64((double(r.m) - f.p.m) * c);
       }
-      t = pick<N>(sw, nseg, u, f);
+      t = pick<kPick, N>(sw, nseg, a.uniforms[int64_t(q) * (D + 1)], f);
     }
   }
   if (threadIdx.x == 0) {
@@ -731,28 +855,29 @@ __global__ __launch_bounds__(256) void chain_final(VerifyArgs a, int nseg, doubl
 constexpr size_t kAlign = 256;
 size_t up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
 
-bool by_level(int, int budget, int, int) { return budget > kWalkNodes; }
+// All rows at once or level by level.
+bool by_level(int, int budget, int, int) { return budget > 256; }
 
 template <bool BF>
 hipError_t tree(const VerifyArgs& a, hipStream_t s) {
   const int nseg = segments(a.vocab);
   const double c = a.inv_t * 1.4426950408889634;
+  hipError_t e;
   if (!by_level(a.batch, a.budget, a.max_len, a.vocab)) {
     Record* rec = static_cast<Record*>(a.ws);
     const int64_t rows = int64_t(a.batch) * (a.budget + 1);
-    hipLaunchKernelGGL(row_records<BF>, dim3(unsigned(rows * nseg)), dim3(256), 0, s, a.target, a.row_stride, a.vocab, nseg, c, rec);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(tree_walk<BF>, dim3(a.batch), dim3(512), 0, s, a, nseg, c, rec);
+    hipLaunchKernelGGL(row_records<BF>, dim3(unsigned(rows * nseg)), dim3(256), 0, s, a.target, rows, nullptr, a.row_stride,
+                       a.vocab, nseg, c, rec, nullptr, 0);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+    hipLaunchKernelGGL(tree_walk<BF>, dim3(a.batch), dim3(kWalkNodes), 0, s, a, nseg, c, rec);
     return hipGetLastError();
   }
   Walk* walk = static_cast<Walk*>(a.ws);
   Record* rec = reinterpret_cast<Record*>(static_cast<char*>(a.ws) + up(a.batch * sizeof(Walk)));
+  hipLaunchKernelGGL(walk_begin, dim3((a.batch + 255) / 256), dim3(256), 0, s, walk, a.batch);
+  if ((e = hipGetLastError()) != hipSuccess) return e;
   for (int level = 0; level <= std::min(a.max_len, a.budget); ++level) {
-    hipLaunchKernelGGL(level_records<BF>, dim3(unsigned(a.batch * nseg)), dim3(256), 0, s, a, nseg, c, walk, rec, level);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(level_step<BF>, dim3(a.batch), dim3(256), 0, s, a, nseg, c, walk, rec, level);
+    hipLaunchKernelGGL(walk_level<BF>, dim3(unsigned(a.batch * nseg)), dim3(kPick), 0, s, a, nseg, c, walk, rec);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
   return hipSuccess;
@@ -764,19 +889,14 @@ hipError_t chain(const VerifyArgs& a, hipStream_t s) {
   const double c = a.inv_t * 1.4426950408889634;
   Record* trec = static_cast<Record*>(a.ws);
   Record* drec = trec + int64_t(a.batch) * (a.budget + 1) * nseg;
-  double* segw = reinterpret_cast<double*>(drec + int64_t(a.batch) * a.budget * nseg);
-  hipLaunchKernelGGL(row_records<BF>, dim3(unsigned(a.batch * (a.budget + 1) * nseg)), dim3(256), 0, s, a.target, a.row_stride,
-                     a.vocab, nseg, c, trec);
-  hipError_t e = hipGetLastError();
+  uint64_t* segw = reinterpret_cast<uint64_t*>(drec + int64_t(a.batch) * a.budget * nseg);
+  int32_t* arrived = reinterpret_cast<int32_t*>(segw + int64_t(a.batch) * nseg);
+  const int64_t trows = int64_t(a.batch) * (a.budget + 1), drows = c != 0.0 ? int64_t(a.batch) * a.budget : 0;
+  hipLaunchKernelGGL(row_records<BF>, dim3(unsigned((trows + drows) * nseg)), dim3(256), 0, s, a.target, trows, a.draft, a.row_stride,
+                     a.vocab, nseg, c, trec, arrived, a.batch);
+  const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  if (c != 0.0) {
-    hipLaunchKernelGGL(row_records<BF>, dim3(unsigned(a.batch * a.budget * nseg)), dim3(256), 0, s, a.draft, a.row_stride, a.vocab,
-                       nseg, c, drec);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
-    hipLaunchKernelGGL(chain_residual<BF>, dim3(nseg, a.batch), dim3(256), 0, s, a, nseg, c, trec, drec, segw);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
-  }
-  hipLaunchKernelGGL(chain_final<BF>, dim3(1, a.batch), dim3(256), 0, s, a, nseg, c, trec, drec, segw);
+  hipLaunchKernelGGL(chain_final<BF>, dim3(c != 0.0 ? nseg : 1, a.batch), dim3(kPick), 0, s, a, nseg, c, trec, drec, segw, arrived);
   return hipGetLastError();
 }
 
@@ -790,7 +910,7 @@ size_t verify_tree_workspace(int batch, int budget, int max_len, int vocab) {
 
 size_t verify_chain_workspace(int batch, int depth, int vocab) {
   const size_t nseg = segments(vocab), b = batch;
-  return up(b * (2 * size_t(depth) + 1) * nseg * sizeof(Record) + b * nseg * sizeof(double));
+  return up(b * (2 * size_t(depth) + 1) * nseg * sizeof(Record) + b * nseg * sizeof(double) + b * sizeof(int32_t));
 }
 
 hipError_t launch_verify_tree(const VerifyArgs& a, hipStream_t s) { return a.bf16 ? tree<true>(a, s) : tree<false>(a, s); }

@@ -73,7 +73,7 @@ dartree_status check_verify(int32_t batch, int32_t budget, int32_t vocab, int32_
   if (!isfinite(t) || t < 0.f) return DARTREE_ERR_INVALID_ARG;
   if (vocab > DARTREE_MAX_VOCAB) return DARTREE_ERR_UNSUPPORTED;
   // (row, segment) blocks are counted in 31 bits
-  if (double(batch) * (budget + 1.0) * (vocab / 4096 + 2) > double(1 << 30) || batch > 65535) return DARTREE_ERR_UNSUPPORTED;
+  if (2.0 * batch * (budget + 1.0) * (vocab / 4096 + 2) > double(1 << 30) || batch > 65535) return DARTREE_ERR_UNSUPPORTED;
   return DARTREE_OK;
 }
 dartree_status check_tree(int32_t batch, int32_t budget, int32_t max_len, int32_t vocab, int32_t type, float t) {
