@@ -102,14 +102,14 @@ __constant__ double kExp32[32] = {
 // The same for the many elements of a pass: exp((z - m) / T) = 2^(n / 32) 2^(f / 32),
 // |f| <= 1/2, from a table in LDS (32 entries take 64 banks: no conflicts) and a
 // series to degree 4 (the next term is below 2e-12).  NaN and -inf give 2^-1000,
-// nothing beside a sum that is at least 1; z above m gives 1.
+// nothing beside a sum that is at least 1.  z is at most m.
 struct ExpTable {
   const double* table;   // LDS
   double c32, mc32;      // 32 log2(e) / T, m times that
   __device__ ExpTable(const double* t, double c, float m) : table(t), c32(32.0 * c), mc32(double(m) * (32.0 * c)) {}
   __device__ void add(float z, double& sum) const {
     constexpr double kRound = 6755399441055744.0;   // 1.5 * 2^52: adding it leaves the nearest whole number in the low bits
-    const double t = fmin(fmax(fma(double(z), c32, -mc32), -32000.0), 0.0);
+    const double t = fmax(fma(double(z), c32, -mc32), -32000.0);
     const double r = t + kRound, f = t - (r - kRound);
     const int n = int(uint32_t(__builtin_bit_cast(uint64_t, r)));
     double p = 9.172562701824643e-09;
@@ -214,10 +214,17 @@ __device__ __forceinline__ void segment_record(const Segment<BF, NT>& in, double
           if (x[l][i] >= m) arg = min(arg, first[l] + i);
     } else {
       const ExpTable e(table, c, m);
+      if (m < 3.40282347e+38f) {
 #pragma unroll
-      for (int l = 0; l < L; ++l)
+        for (int l = 0; l < L; ++l)
 #pragma unroll
-        for (int i = 0; i < N; ++i) e.add(x[l][i], s);
+          for (int i = 0; i < N; ++i) e.add(x[l][i], s);
+      } else {   // +inf counts as the largest number
+#pragma unroll
+        for (int l = 0; l < L; ++l)
+#pragma unroll
+          for (int i = 0; i < N; ++i) e.add(sane(x[l][i]), s);
+      }
     }
   }
   if (c == 0.0) {
