@@ -145,17 +145,13 @@ struct Chunk {   // 32 keys and values as read
   u32x4 k[2][E8 ? 2 : 4];
   u32x2 v8[E8 ? 8 : 1];
   u32x4 v16[E8 ? 1 : 8];
-  uint8_t ke[2];
+  uint32_t ke[2];
   u32x2 ve;
 };
 
-// S, softmax and O of one chunk.  vis: bit 8 g + i set where lane group g's key i
-// is seen by row group r's query (masked: some bit is clear).
+// Scores of a chunk.
 template <int RG, bool E8>
-__device__ __forceinline__ void chunk_step(const Chunk<RG, E8>& c, const u32x4 (&qf)[RG][4], const bool masked,
-                                           const uint32_t (&vis)[RG], const uint32_t there, const float c2, Rows<RG>& st) {
-  const int g = (threadIdx.x & 63) >> 4;
-  f32x4 s[RG][2];
+__device__ __forceinline__ void chunk_scores(const Chunk<RG, E8>& c, const u32x4 (&qf)[RG][4], f32x4 (&s)[RG][2]) {
 #pragma unroll
   for (int t = 0; t < 2; ++t) {
 #pragma unroll
@@ -174,6 +170,14 @@ __device__ __forceinline__ void chunk_step(const Chunk<RG, E8>& c, const u32x4 (
       for (int r = 0; r < RG; ++r) s[r][t] = mfma16(kf, qf[r][ks], s[r][t]);
     }
   }
+}
+
+// Weights of a chunk from its scores.  vis: bit 8 g + i set where lane group g's key
+// i is seen by row group r's query (masked: some bit is clear).
+template <int RG>
+__device__ __forceinline__ void chunk_weights(f32x4 (&s)[RG][2], const bool masked, const uint32_t (&vis)[RG], const float c2,
+                                              Rows<RG>& st, u32x4 (&p)[RG]) {
+  const int g = (threadIdx.x & 63) >> 4;
   if (masked) {
 #pragma unroll
     for (int r = 0; r < RG; ++r) {
@@ -188,7 +192,6 @@ __device__ __forceinline__ void chunk_step(const Chunk<RG, E8>& c, const u32x4 (
   // The reference m of a row moves only when a key exceeds it by more than 2^8,
   // so most chunks need no exchange between lanes and no rescaling; weights
   // stay below 2^8 and a row that has seen no key keeps m = -inf, l = 0, O = 0.
-  u32x4 p[RG];
 #pragma unroll
   for (int r = 0; r < RG; ++r) {
     float top = -INFINITY;
@@ -221,8 +224,13 @@ __device__ __forceinline__ void chunk_step(const Chunk<RG, E8>& c, const u32x4 (
       for (int i = 0; i < 4; ++i) w[4 * t + i] = __bf16(s[r][t][i]);
     p[r] = __builtin_bit_cast(u32x4, w);
   }
-  // V: dims 8 c + 2 j, 8 c + 2 j + 1 of eight keys, transposed.  A key that is
-  // not there has zeros instead of what its memory holds: 0 * NaN is NaN.
+}
+
+// O of a chunk.  V: dims 8 c + 2 j, 8 c + 2 j + 1 of eight keys, transposed.  A key
+// that is not there has zeros instead of what its memory holds: 0 * NaN is NaN.
+template <int RG, bool E8>
+__device__ __forceinline__ void chunk_values(const Chunk<RG, E8>& c, const uint32_t there, const u32x4 (&p)[RG], Rows<RG>& st) {
+  const int g = (threadIdx.x & 63) >> 4;
   const uint32_t here = there >> (8 * g);
   const bool whole = there == ~0u;
 #pragma unroll
@@ -309,60 +317,79 @@ __global__ __launch_bounds__(256, RG == 1 ? 2 : 1) void paged_attention(PagedArg
       for (int t = 0; t < 8; ++t) st.o[r][t] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
 
-    // context: chunk of keys kb .. kb + 31
+    // The context: chunks of keys kb .. kb + 31, a step apart.  The next chunk's keys
+    // are fetched once this one's scores are formed, its values once this one's
+    // are added, so a chunk's bytes are in flight all the time.
     const Uniform table = uniform_array(a.c.table) + int64_t(q) * a.c.max_pages;
-    auto pages_of = [&](int kb, int& p0, int& p1) {   // pages of the chunk's halves; -1: none
-      p0 = table[kb >> a.c.page_log2];
-      p0 = p0 < a.c.num_pages ? p0 : -1;
-      const int k1 = kb + 16;
-      p1 = k1 < ex.ctx ? table[k1 >> a.c.page_log2] : -1;
-      p1 = p1 < a.c.num_pages ? p1 : -1;
-    };
-    const int end = min(step + n, nctx);
-    for (int s = step; s < end; ++s) {
-      const int kb = s * kStep + wave * kChunk;
-      if (kb >= ex.ctx) break;
-      int p0, p1;
-      pages_of(kb, p0, p1);
-      if (p0 < 0 && p1 < 0) continue;
-      const int valid = min(kChunk, ex.ctx - kb);
-      uint32_t there = valid == 32 ? ~0u : (1u << valid) - 1u;
-      if (p0 < 0) there &= 0xFFFF0000u;
-      if (p1 < 0) there &= 0x0000FFFFu;
-      const int h0 = p0 < 0 ? p1 : p0, h1 = p1 < 0 ? p0 : p1;   // a page to read from in any case
-      auto row_of = [&](int key) {
-        const int64_t page = key < 16 ? h0 : h1;
-        return ((page * a.heads_kv + kvh) << a.c.page_log2) + ((kb + key) & (page_size - 1));
-      };
+    const int kb0 = step * kStep + wave * kChunk;
+    const int chunks = kb0 < ex.ctx ? min(min(step + n, nctx) - step, (ex.ctx - kb0 + kStep - 1) / kStep) : 0;
+    if (chunks > 0) {
       Chunk<RG, E8> ch;
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        const int64_t row = row_of(8 * (c16 >> 2) + 4 * t + (c16 & 3));
-        if constexpr (E8) {
-          const uint8_t* kp = static_cast<const uint8_t*>(a.c.k) + row * kHead + 16 * g;
-          ch.k[t][0] = *reinterpret_cast<const u32x4*>(kp);
-          ch.k[t][1] = *reinterpret_cast<const u32x4*>(kp + 64);
-          ch.ke[t] = a.c.k_exp[row];
-        } else {
-          const uint16_t* kp = static_cast<const uint16_t*>(a.c.k) + row * kHead + 16 * g;
-#pragma unroll
-          for (int ks = 0; ks < 4; ++ks)
-            ch.k[t][ks] = *reinterpret_cast<const u32x4*>(kp + 64 * (ks >> 1) + 8 * (ks & 1));
-        }
-      }
-      const int64_t vrow = row_of(8 * g);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        if constexpr (E8)
-          ch.v8[e] = *reinterpret_cast<const u32x2*>(static_cast<const uint8_t*>(a.c.v) + (vrow + e) * kHead + 8 * c16);
-        else
-          ch.v16[e] = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(a.c.v) + (vrow + e) * kHead + 8 * c16);
-      }
-      if constexpr (E8) ch.ve = *reinterpret_cast<const u32x2*>(a.c.v_exp + vrow);
+      f32x4 sc[RG][2];
+      u32x4 p[RG];
       uint32_t vis[RG];
+      int p0, p1;   // pages of the halves of the chunk to fetch next
+      auto look_up = [&](int kb) __attribute__((always_inline)) {
+        p0 = table[kb >> a.c.page_log2];
+        p1 = table[min(kb + 16, ex.ctx - 1) >> a.c.page_log2];
+      };
+      int64_t vrow = 0;
+      uint32_t next = 0;   // which keys of the fetched chunk are there
+      auto fetch_keys = [&](int kb) __attribute__((always_inline)) {
+        const int valid = min(kChunk, ex.ctx - kb);
+        next = valid == 32 ? ~0u : (1u << valid) - 1u;
+        const bool in0 = uint32_t(p0) < uint32_t(a.c.num_pages), in1 = uint32_t(p1) < uint32_t(a.c.num_pages);
+        if (!in0) next &= 0xFFFF0000u;
+        if (!in1) next &= 0x0000FFFFu;
+        const int h0 = in0 ? p0 : 0, h1 = in1 ? p1 : 0;   // any page: what is read is not used
+        auto row_of = [&](int key) {
+          const int64_t page = key < 16 ? h0 : h1;
+          return ((page * a.heads_kv + kvh) << a.c.page_log2) + ((kb + key) & (page_size - 1));
+        };
 #pragma unroll
-      for (int r = 0; r < RG; ++r) vis[r] = there;
-      chunk_step<RG, E8>(ch, qf, there != ~0u, vis, there, a.scale_log2, st);
+        for (int t = 0; t < 2; ++t) {
+          const int64_t row = row_of(8 * (c16 >> 2) + 4 * t + (c16 & 3));
+          if constexpr (E8) {
+            const uint8_t* kp = static_cast<const uint8_t*>(a.c.k) + row * kHead + 16 * g;
+            ch.k[t][0] = *reinterpret_cast<const u32x4*>(kp);
+            ch.k[t][1] = *reinterpret_cast<const u32x4*>(kp + 64);
+            ch.ke[t] = a.c.k_exp[row];
+          } else {
+            const uint16_t* kp = static_cast<const uint16_t*>(a.c.k) + row * kHead + 16 * g;
+#pragma unroll
+            for (int ks = 0; ks < 4; ++ks)
+              ch.k[t][ks] = *reinterpret_cast<const u32x4*>(kp + 64 * (ks >> 1) + 8 * (ks & 1));
+          }
+        }
+        vrow = row_of(8 * g);
+      };
+      auto fetch_values = [&] __attribute__((always_inline)) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          if constexpr (E8)
+            ch.v8[e] = *reinterpret_cast<const u32x2*>(static_cast<const uint8_t*>(a.c.v) + (vrow + e) * kHead + 8 * c16);
+          else
+            ch.v16[e] = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(a.c.v) + (vrow + e) * kHead + 8 * c16);
+        }
+        if constexpr (E8) ch.ve = *reinterpret_cast<const u32x2*>(a.c.v_exp + vrow);
+      };
+      look_up(kb0);
+      fetch_keys(kb0);
+      fetch_values();
+#pragma unroll 1
+      for (int i = 0; i < chunks; ++i) {
+        const uint32_t there = next;
+        const int kb = kb0 + (i + 1) * kStep;
+        const bool more = i + 1 < chunks;
+        if (more) look_up(kb);
+        chunk_scores<RG, E8>(ch, qf, sc);
+        if (more) fetch_keys(kb);
+#pragma unroll
+        for (int r = 0; r < RG; ++r) vis[r] = there;
+        chunk_weights<RG>(sc, there != ~0u, vis, a.scale_log2, st, p);
+        chunk_values<RG, E8>(ch, there, p, st);
+        if (more) fetch_values();
+      }
     }
     // the tree's own keys
     for (int s = max(step, nctx); s < step + n; ++s) {
@@ -390,7 +417,11 @@ __global__ __launch_bounds__(256, RG == 1 ? 2 : 1) void paged_attention(PagedArg
         if (mrow[r]) vis[r] = mrow[r][kb >> 5] & there;
         else vis[r] = node[r] < kb ? 0u : (node[r] - kb >= 31 ? ~0u : (2u << (node[r] - kb)) - 1u) & there;
       }
-      chunk_step<RG, false>(ch, qf, true, vis, there, a.scale_log2, st);
+      f32x4 sc[RG][2];
+      u32x4 p[RG];
+      chunk_scores<RG, false>(ch, qf, sc);
+      chunk_weights<RG>(sc, true, vis, a.scale_log2, st, p);
+      chunk_values<RG, false>(ch, there, p, st);
     }
 
     // join the four waves: their rows scaled to the block's maximum, added in wave order
@@ -562,7 +593,7 @@ __global__ __launch_bounds__(256, 2) void paged_tiles(PagedArgs a, int whole) {
         }
       }
     };
-    // unseen keys out; the reference of a row moves as in chunk_step, one test for all rows
+    // unseen keys out; the reference of a row moves as in chunk_weights, one test for all rows
     auto settle = [&](bool masked, const uint32_t (&vis)[RG], f32x4 (&sc)[RG][2]) __attribute__((always_inline)) {
       if (masked) {
 #pragma unroll
