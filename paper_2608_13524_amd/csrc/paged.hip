@@ -8,16 +8,17 @@
 // item cut by a block's end leaves partial results, which a second launch joins
 // in block order.
 //
-// Up to 16 query rows of a key/value head (paged_attention): a step is 128 keys,
-// a chunk of 32 for each of the block's four waves, and a wave works from
-// registers alone.  S^T = K Q^T: row r of the two 16-key tiles is key
-// 8 (r / 4) + 4 t + r % 4, which leaves lane (c = lane % 16, g = lane / 16) with
-// query c's weights of keys 8 g .. 8 g + 7 in order, the B operand of O^T = V^T P^T.
-// For V a lane reads eight dims, 8 c .. 8 c + 7, of those same keys and
-// transposes them in registers; column tile t of the product is then dims 8 c + t,
-// and a lane ends with dims 32 g .. 32 g + 31 of its query.  Keys in e4m3 become
-// bf16 on the way with their power of two applied by the conversion (exact).
-// Every key and value byte is read once and never passes through LDS.
+// Up to 16 query rows of a key/value head, or few keys (paged_attention): a step
+// is a chunk of 32 keys for each of the block's four or eight waves, and a wave
+// works from registers alone.  S^T = K Q^T leaves lane (c = lane % 16, g = lane / 16) with
+// query c's weights of keys 4 g .. 4 g + 3 of both 16-key tiles, the B operand of
+// O^T = V^T P^T with the keys taken in that order.  For V a lane reads eight dims,
+// 8 c .. 8 c + 7, of those same keys and transposes them in registers; column tile
+// t of the product is then dims 8 c + t, and a lane ends with dims 32 g .. 32 g + 31
+// of its query.  A tile lies in one page, so every load has a scalar base and an
+// offset that is the lane's own.  Keys in e4m3 become bf16 on the way with their
+// power of two applied by the conversion (exact).  Every key and value byte is
+// read once and never passes through LDS.
 //
 // More rows (paged_tiles): below.
 #include <algorithm>
@@ -32,8 +33,6 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kChunk = 32;            // keys of a wave's share of a step
-constexpr int kWaves = 4;
-constexpr int kStep = kChunk * kWaves;
 
 __device__ __forceinline__ f32x4 mfma16(u32x4 a, u32x4 b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
@@ -172,8 +171,8 @@ __device__ __forceinline__ void chunk_scores(const Chunk<RG, E8>& c, const u32x4
   }
 }
 
-// Weights of a chunk from its scores.  vis: bit 8 g + i set where lane group g's key
-// i is seen by row group r's query (masked: some bit is clear).
+// Weights of a chunk from its scores.  vis: bit k set where row group r's query sees
+// key k (masked: some bit is clear).
 template <int RG>
 __device__ __forceinline__ void chunk_weights(f32x4 (&s)[RG][2], const bool masked, const uint32_t (&vis)[RG], const float c2,
                                               Rows<RG>& st, u32x4 (&p)[RG]) {
@@ -181,12 +180,12 @@ __device__ __forceinline__ void chunk_weights(f32x4 (&s)[RG][2], const bool mask
   if (masked) {
 #pragma unroll
     for (int r = 0; r < RG; ++r) {
-      const uint32_t b = vis[r] >> (8 * g);
+      const uint32_t b = vis[r] >> (4 * g);
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          if (!((b >> (4 * t + i)) & 1u)) s[r][t][i] = -INFINITY;
+          if (!((b >> (16 * t + i)) & 1u)) s[r][t][i] = -INFINITY;
     }
   }
   // The reference m of a row moves only when a key exceeds it by more than 2^8,
@@ -231,7 +230,7 @@ __device__ __forceinline__ void chunk_weights(f32x4 (&s)[RG][2], const bool mask
 template <int RG, bool E8>
 __device__ __forceinline__ void chunk_values(const Chunk<RG, E8>& c, const uint32_t there, const u32x4 (&p)[RG], Rows<RG>& st) {
   const int g = (threadIdx.x & 63) >> 4;
-  const uint32_t here = there >> (8 * g);
+  const uint32_t here = there >> (4 * g);
   const bool whole = there == ~0u;
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
@@ -245,7 +244,7 @@ __device__ __forceinline__ void chunk_values(const Chunk<RG, E8>& c, const uint3
       } else {
         w[e] = c.v16[e][j];
       }
-      if (!whole) w[e] = (here >> e) & 1u ? w[e] : 0u;
+      if (!whole) w[e] = (here >> (16 * (e >> 2) + (e & 3))) & 1u ? w[e] : 0u;
     }
     u32x4 lo, hi;
 #pragma unroll
@@ -275,8 +274,9 @@ __device__ __forceinline__ Parts parts_of(const PagedArgs& a, int blocks) {
   return Parts{o, o + int64_t(blocks) * 2 * ROWS * kHead};
 }
 
-template <int RG, bool E8>
-__global__ __launch_bounds__(256, RG == 1 ? 2 : 1) void paged_attention(PagedArgs a, int whole) {
+template <int RG, bool E8, int W>
+__global__ __launch_bounds__(64 * W, RG == 1 ? 8 / W : 1) void paged_attention(PagedArgs a, int whole) {
+  constexpr int kWaves = W, kStep = kChunk * W;
   __shared__ __attribute__((aligned(16))) float red[kWaves * RG * 8 * 64 * 4];
   __shared__ float ml[kWaves][16 * RG][2];
   const int lane = threadIdx.x & 63, c16 = lane & 15, g = lane >> 4;
@@ -333,45 +333,43 @@ __global__ __launch_bounds__(256, RG == 1 ? 2 : 1) void paged_attention(PagedArg
         p0 = table[kb >> a.c.page_log2];
         p1 = table[min(kb + 16, ex.ctx - 1) >> a.c.page_log2];
       };
-      int64_t vrow = 0;
-      uint32_t next = 0;   // which keys of the fetched chunk are there
+      int64_t row0[2] = {0, 0};   // the tiles' first rows
+      uint32_t next = 0;          // which keys of the fetched chunk are there
+      const int koff = E8 ? c16 * kHead + 16 * g : c16 * 2 * kHead + 32 * g, voff = E8 ? 4 * g * kHead + 8 * c16 : 4 * g * 2 * kHead + 16 * c16;
       auto fetch_keys = [&](int kb) __attribute__((always_inline)) {
         const int valid = min(kChunk, ex.ctx - kb);
         next = valid == 32 ? ~0u : (1u << valid) - 1u;
         const bool in0 = uint32_t(p0) < uint32_t(a.c.num_pages), in1 = uint32_t(p1) < uint32_t(a.c.num_pages);
         if (!in0) next &= 0xFFFF0000u;
         if (!in1) next &= 0x0000FFFFu;
-        const int h0 = in0 ? p0 : 0, h1 = in1 ? p1 : 0;   // any page: what is read is not used
-        auto row_of = [&](int key) {
-          const int64_t page = key < 16 ? h0 : h1;
-          return ((page * a.heads_kv + kvh) << a.c.page_log2) + ((kb + key) & (page_size - 1));
-        };
+        const int64_t h0 = in0 ? p0 : 0, h1 = in1 ? p1 : 0;   // any page: what is read is not used
+        row0[0] = ((h0 * a.heads_kv + kvh) << a.c.page_log2) + (kb & (page_size - 1));
+        row0[1] = ((h1 * a.heads_kv + kvh) << a.c.page_log2) + ((kb + 16) & (page_size - 1));
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-          const int64_t row = row_of(8 * (c16 >> 2) + 4 * t + (c16 & 3));
+          const char* kp = static_cast<const char*>(a.c.k) + row0[t] * (E8 ? kHead : 2 * kHead);
           if constexpr (E8) {
-            const uint8_t* kp = static_cast<const uint8_t*>(a.c.k) + row * kHead + 16 * g;
-            ch.k[t][0] = *reinterpret_cast<const u32x4*>(kp);
-            ch.k[t][1] = *reinterpret_cast<const u32x4*>(kp + 64);
-            ch.ke[t] = a.c.k_exp[row];
+            ch.k[t][0] = *reinterpret_cast<const u32x4*>(kp + koff);
+            ch.k[t][1] = *reinterpret_cast<const u32x4*>(kp + koff + 64);
+            ch.ke[t] = (a.c.k_exp + row0[t])[c16];
           } else {
-            const uint16_t* kp = static_cast<const uint16_t*>(a.c.k) + row * kHead + 16 * g;
 #pragma unroll
             for (int ks = 0; ks < 4; ++ks)
-              ch.k[t][ks] = *reinterpret_cast<const u32x4*>(kp + 64 * (ks >> 1) + 8 * (ks & 1));
+              ch.k[t][ks] = *reinterpret_cast<const u32x4*>(kp + koff + 128 * (ks >> 1) + 16 * (ks & 1));
           }
         }
-        vrow = row_of(8 * g);
       };
       auto fetch_values = [&] __attribute__((always_inline)) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          if constexpr (E8)
-            ch.v8[e] = *reinterpret_cast<const u32x2*>(static_cast<const uint8_t*>(a.c.v) + (vrow + e) * kHead + 8 * c16);
-          else
-            ch.v16[e] = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(a.c.v) + (vrow + e) * kHead + 8 * c16);
+          const char* vp = static_cast<const char*>(a.c.v) + row0[e >> 2] * (E8 ? kHead : 2 * kHead);
+          if constexpr (E8) ch.v8[e] = *reinterpret_cast<const u32x2*>(vp + voff + (e & 3) * kHead);
+          else ch.v16[e] = *reinterpret_cast<const u32x4*>(vp + voff + (e & 3) * 2 * kHead);
         }
-        if constexpr (E8) ch.ve = *reinterpret_cast<const u32x2*>(a.c.v_exp + vrow);
+        if constexpr (E8) {
+#pragma unroll
+          for (int t = 0; t < 2; ++t) ch.ve[t] = *reinterpret_cast<const uint32_t*>(a.c.v_exp + row0[t] + 4 * g);
+        }
       };
       look_up(kb0);
       fetch_keys(kb0);
@@ -403,14 +401,14 @@ __global__ __launch_bounds__(256, RG == 1 ? 2 : 1) void paged_attention(PagedArg
       Chunk<RG, false> ch;
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
-        const uint16_t* kp = a.k_tree + at(8 * (c16 >> 2) + 4 * t + (c16 & 3)) + 16 * g;
+        const uint16_t* kp = a.k_tree + at(16 * t + c16) + 16 * g;
 #pragma unroll
         for (int ks = 0; ks < 4; ++ks)
           ch.k[t][ks] = *reinterpret_cast<const u32x4*>(kp + 64 * (ks >> 1) + 8 * (ks & 1));
       }
 #pragma unroll
       for (int e = 0; e < 8; ++e)
-        ch.v16[e] = *reinterpret_cast<const u32x4*>(a.v_tree + at(8 * g + e) + 8 * c16);
+        ch.v16[e] = *reinterpret_cast<const u32x4*>(a.v_tree + at(16 * (e >> 2) + 4 * g + (e & 3)) + 8 * c16);
       uint32_t vis[RG];
 #pragma unroll
       for (int r = 0; r < RG; ++r) {
@@ -444,8 +442,10 @@ __global__ __launch_bounds__(256, RG == 1 ? 2 : 1) void paged_attention(PagedArg
     __syncthreads();
     const bool direct = n == steps;
     const int slot = 2 * blk + (step > 0 ? 0 : 1);
+    const int i4 = wave & 3;   // this wave: dims 32 g + 8 i4 .. + 7 of row groups wave / 4, + W / 4, ..
 #pragma unroll
-    for (int r = 0; r < RG; ++r) {   // this wave: dims 32 g + 8 wave .. + 7 of every row
+    for (int r = 0; r < RG; ++r) {
+      if (r % (W / 4) != wave / 4) continue;
       const int lr = r * 16 + c16, row = rt * 16 * RG + lr;
       float M = ml[0][lr][0];
 #pragma unroll
@@ -459,7 +459,7 @@ __global__ __launch_bounds__(256, RG == 1 ? 2 : 1) void paged_attention(PagedArg
         L += f * ml[w][lr][1];
 #pragma unroll
         for (int h = 0; h < 2; ++h)
-          v[h] += f * *reinterpret_cast<const f32x4*>(&red[(((w * RG + r) * 8 + 2 * wave + h) * 64 + lane) * 4]);
+          v[h] += f * *reinterpret_cast<const f32x4*>(&red[(((w * RG + r) * 8 + 2 * i4 + h) * 64 + lane) * 4]);
       }
       if (row < rows) {
         if (direct) {
@@ -469,12 +469,12 @@ __global__ __launch_bounds__(256, RG == 1 ? 2 : 1) void paged_attention(PagedArg
           for (int i = 0; i < 8; ++i) o[i] = __bf16(v[i >> 2][i & 3] * inv);
           const int nd = row / a.group;
           const int64_t head = (int64_t(q) * a.budget + nd) * a.heads_q + kvh * a.group + row - nd * a.group;
-          *reinterpret_cast<bf16x8*>(a.out + head * kHead + 32 * g + 8 * wave) = o;
+          *reinterpret_cast<bf16x8*>(a.out + head * kHead + 32 * g + 8 * i4) = o;
         } else {
-          float* po = parts.o + (int64_t(slot) * 16 * RG + lr) * kHead + 32 * g + 8 * wave;
+          float* po = parts.o + (int64_t(slot) * 16 * RG + lr) * kHead + 32 * g + 8 * i4;
           *reinterpret_cast<f32x4*>(po) = v[0];
           *reinterpret_cast<f32x4*>(po + 4) = v[1];
-          if (wave == 0 && g == 0) {
+          if (i4 == 0 && g == 0) {
             parts.ml[(int64_t(slot) * 16 * RG + lr) * 2] = M;
             parts.ml[(int64_t(slot) * 16 * RG + lr) * 2 + 1] = L;
           }
@@ -931,33 +931,50 @@ __global__ __launch_bounds__(256) void paged_join(PagedArgs a, int blocks) {
   *reinterpret_cast<bf16x4*>(out) = bf16x4{__bf16(acc[0] * inv), __bf16(acc[1] * inv), __bf16(acc[2] * inv), __bf16(acc[3] * inv)};
 }
 
-// Which kernel (tiles: paged_tiles, else paged_attention), its tile's query rows
-// and the blocks of a launch: as many as the chip holds, sharing the line of
-// steps, or one per item where there are plenty.
+// Which kernel, its tile's query rows and the blocks of a launch: as many as the
+// chip holds, sharing the line of steps, or one per item.
+enum Kernel { kFew, kFewWhole, kTiles64, kTiles128 };
 struct Plan {
-  int tiles, rows, blocks, whole;
+  Kernel kernel;
+  int rows, blocks, whole;
   int64_t items;
 };
-Plan plan_of(int batch, int budget, int max_ctx, int heads_q, int heads_kv) {
-  constexpr int kResident = 512;   // two blocks a compute unit
+Plan plan_of(int batch, int budget, int max_ctx, int heads_q, int heads_kv, int eight) {
+  constexpr int kResident = 512;   // two blocks of four waves a compute unit
   const int rows = budget * (heads_q / heads_kv);
-  Plan p{};
-  p.tiles = rows > 16;
-  const int step = p.tiles ? kTile : kStep;
-  const int64_t steps = std::max(1, (max_ctx + step - 1) / step + (budget + step - 1) / step);
   const int64_t heads = int64_t(batch) * heads_kv;
+  auto tiles_of = [&](int n) { return heads * ((rows + n - 1) / n); };
+  Plan p{};
+  // Few 16-row items with few keys: a block of eight waves takes each, with no
+  // partial results and no second launch.  A compute unit draws about 47 GB/s,
+  // 1.4 us per 256 keys of e4m3.  Whole / shared (us, 32 / 8 heads, e4m3 unless
+  // said): 1 request x 64 nodes, 512 positions 10 / 18, 2048 20 / 22 (bf16 25 /
+  // 22), 4096 32 / 26; 4 x 64 x 1024 26 / 27, 8 x 64 x 1024 48 / 36; 4 x 16 x
+  // 2048 20 / 23; single tokens: 1 x 512 9 / 10, 1 x 2048 18 / 12, 4 x 2048 19 /
+  // 15, 16 x 2048 19 / 21.
+  const int64_t turns = ((int64_t(max_ctx) + budget + 255) / 256) * (eight ? 1 : 2), few = tiles_of(16);
+  if (few <= 512 && (turns <= 3 || (turns <= 4 && rows > 16) || (turns <= 9 && few <= 256 && (rows > 16 || few >= 128)))) {
+    p.kernel = kFewWhole;
+    p.rows = 16;
+    p.items = p.blocks = int(few);
+    p.whole = 1;
+    return p;
+  }
+  const int step = rows <= 16 ? 128 : kTile;
+  const int64_t steps = (int64_t(max_ctx) + step - 1) / step + (budget + step - 1) / step;
   // 128 rows a tile double a tile's products per byte from LDS, and a cut item's
   // partial results; worth it where blocks take eight steps and more
-  p.rows = !p.tiles ? 16 : rows <= 64 || heads * ((rows + 127) / 128) * steps < 8 * kResident ? 64 : 128;
-  p.items = heads * ((rows + p.rows - 1) / p.rows);
+  p.kernel = rows <= 16 ? kFew : rows <= 64 || tiles_of(128) * steps < 8 * kResident ? kTiles64 : kTiles128;
+  p.rows = p.kernel == kFew ? 16 : p.kernel == kTiles64 ? 64 : 128;
+  p.items = tiles_of(p.rows);
   p.whole = p.items >= 4 * kResident;
   p.blocks = int(p.whole ? p.items : std::min<int64_t>(kResident, p.items * steps));
   return p;
 }
 
-template <int ROWS, int STEP, typename K>
+template <int ROWS, int STEP, int THREADS = 256, typename K>
 hipError_t launch(K* kernel, const PagedArgs& a, const Plan& p, hipStream_t s) {
-  hipLaunchKernelGGL(kernel, dim3(p.blocks), dim3(256), 0, s, a, p.whole);
+  hipLaunchKernelGGL(kernel, dim3(p.blocks), dim3(THREADS), 0, s, a, p.whole);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.whole) return e;
   hipLaunchKernelGGL((paged_join<ROWS, STEP>), dim3(unsigned(p.items * (ROWS / 8))), dim3(256), 0, s, a, p.blocks);
@@ -966,16 +983,24 @@ hipError_t launch(K* kernel, const PagedArgs& a, const Plan& p, hipStream_t s) {
 
 }  // namespace
 
-size_t paged_attention_workspace(int batch, int budget, int max_ctx, int heads_q, int heads_kv, int) {
-  const Plan p = plan_of(batch, budget, max_ctx, heads_q, heads_kv);
+size_t paged_attention_workspace(int batch, int budget, int max_ctx, int heads_q, int heads_kv, int eight) {
+  const Plan p = plan_of(batch, budget, max_ctx, heads_q, heads_kv, eight);
   return p.whole ? 0 : size_t(p.blocks) * 2 * p.rows * (kHead + 2) * sizeof(float);
 }
 
 hipError_t launch_paged_attention(const PagedArgs& a, hipStream_t s) {
-  const Plan p = plan_of(a.batch, a.budget, a.max_ctx, a.heads_q, a.heads_kv);
-  if (!p.tiles) return a.eight ? launch<16, kStep>(paged_attention<1, true>, a, p, s) : launch<16, kStep>(paged_attention<1, false>, a, p, s);
-  if (p.rows == 64) return a.eight ? launch<64, kTile>(paged_tiles<1, true>, a, p, s) : launch<64, kTile>(paged_tiles<1, false>, a, p, s);
-  return a.eight ? launch<128, kTile>(paged_tiles<2, true>, a, p, s) : launch<128, kTile>(paged_tiles<2, false>, a, p, s);
+  const Plan p = plan_of(a.batch, a.budget, a.max_ctx, a.heads_q, a.heads_kv, a.eight);
+  switch (p.kernel) {
+    case kFew:
+      return a.eight ? launch<16, 128>(paged_attention<1, true, 4>, a, p, s) : launch<16, 128>(paged_attention<1, false, 4>, a, p, s);
+    case kFewWhole:
+      return a.eight ? launch<16, 256, 512>(paged_attention<1, true, 8>, a, p, s)
+                     : launch<16, 256, 512>(paged_attention<1, false, 8>, a, p, s);
+    case kTiles64:
+      return a.eight ? launch<64, kTile>(paged_tiles<1, true>, a, p, s) : launch<64, kTile>(paged_tiles<1, false>, a, p, s);
+    default:
+      return a.eight ? launch<128, kTile>(paged_tiles<2, true>, a, p, s) : launch<128, kTile>(paged_tiles<2, false>, a, p, s);
+  }
 }
 
 }  // namespace dartree
