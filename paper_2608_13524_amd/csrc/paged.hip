@@ -38,6 +38,15 @@ __device__ __forceinline__ f32x4 mfma16(u32x4 a, u32x4 b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
 
+// sum += eight bf16 weights, in 32 bits: the rounded ones, as they multiply the
+// values, so that a common rounding cancels; two a lane and instruction.
+__device__ __forceinline__ void add_weights(u32x4 w, float& sum) {
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  const bf16x2 ones = __builtin_bit_cast(bf16x2, 0x3F803F80u);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, uint32_t(w[i])), ones, sum, false);
+}
+
 template <bool HI>
 __device__ __forceinline__ uint32_t expand2(uint32_t w, float scale) {
   return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, HI));
@@ -209,19 +218,13 @@ __device__ __forceinline__ void chunk_weights(f32x4 (&s)[RG][2], const bool mask
       st.m[r] = m;
     }
     const float ref = -(st.m[r] == -INFINITY ? 0.f : st.m[r]) * c2;
-#pragma unroll
-    for (int t = 0; t < 2; ++t)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        s[r][t][i] = __builtin_amdgcn_exp2f(fmaf(s[r][t][i], c2, ref));
-        st.l[r] += s[r][t][i];
-      }
     bf16x8 w;
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) w[4 * t + i] = __bf16(s[r][t][i]);
+      for (int i = 0; i < 4; ++i) w[4 * t + i] = __bf16(__builtin_amdgcn_exp2f(fmaf(s[r][t][i], c2, ref)));
     p[r] = __builtin_bit_cast(u32x4, w);
+    add_weights(p[r], st.l[r]);
   }
 }
 
@@ -493,8 +496,8 @@ __global__ __launch_bounds__(64 * W, RG == 1 ? 8 / W : 1) void paged_attention(P
 }
 
 // ---------------------------------------------------------------------------
-// Many rows: a block's four waves hold 16 RG query rows each and share tiles of
-// 64 keys through LDS, in bf16 (e4m3 is converted once, as it is stored).  Tile
+// Many rows: a block's W waves hold 16 RG query rows each and share tiles of 64
+// keys through LDS, in bf16 (e4m3 is converted once, as it is stored).  Tile
 // s + 1 travels in registers while tile s is multiplied, in two buffers.  A row
 // of 256 bytes keeps its 16-byte chunk c at c ^ k_place or c ^ v_place of the
 // row: K is read a row per lane, V transposed (ds_read_b64_tr_b16: lane l gets dim
@@ -527,11 +530,11 @@ struct Index {
   static constexpr int value = N;
 };
 
-template <int RG, bool E8>
-__global__ __launch_bounds__(256, 2) void paged_tiles(PagedArgs a, int whole) {
+template <int RG, bool E8, int W>
+__global__ __launch_bounds__(64 * W, 8 / W) void paged_tiles(PagedArgs a, int whole) {
   __shared__ __attribute__((aligned(16))) char smem[4 * kTileBytes];   // [buffer][K, V]
   LDS_AS char* const lds = (LDS_AS char*)smem;
-  constexpr int kRows = 64 * RG;
+  constexpr int kRows = 16 * W * RG;
   const int lane = threadIdx.x & 63, r16 = lane & 15, g = lane >> 4;
   const int wave = uniform(threadIdx.x >> 6);
   const int rows = a.budget * a.group, ntile = (rows + kRows - 1) / kRows;
@@ -638,12 +641,9 @@ __global__ __launch_bounds__(256, 2) void paged_tiles(PagedArgs a, int whole) {
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float e = __builtin_amdgcn_exp2f(fmaf(sc[r][t][i], c2, ref[r]));
-            l[r] += e;
-            w[4 * t + i] = __bf16(e);
-          }
+          for (int i = 0; i < 4; ++i) w[4 * t + i] = __bf16(__builtin_amdgcn_exp2f(fmaf(sc[r][t][i], c2, ref[r])));
         p[r] = __builtin_bit_cast(u32x4, w);
+        add_weights(p[r], l[r]);
       }
     };
     auto values = [&](auto B, auto C, const u32x4 (&p)[RG]) __attribute__((always_inline)) {
@@ -708,32 +708,28 @@ __global__ __launch_bounds__(256, 2) void paged_tiles(PagedArgs a, int whole) {
 
     {   // the context
       const int32_t* table = a.c.table + int64_t(q) * a.c.max_pages;
-      constexpr int kShares = E8 ? 2 : 4;
+      constexpr int kRowsWave = E8 ? 8 : 4, kShares = kTile / (kRowsWave * W);
       u32x4 kx[kShares], vx[kShares];
-      uint32_t ke[2], ve[2];
+      uint32_t ke[kShares], ve[kShares];
       uint64_t in_flight = 0;
       int page;   // lane i % 4: the page of the i-th 16 keys of the tile to fetch next
       auto look_up = [&](int s) __attribute__((always_inline)) {
         page = table[min(s * kTile + 16 * (thread_again() & 3), ex.ctx - 1) >> a.c.page_log2];
       };
-      // a wave's keys of a share lie in one group of 16, so in one page: in e4m3
-      // eight rows of 128 bytes, keys 32 i + 8 wave ..; in bf16 four of 256, 16 i + 4 wave ..
+      // a wave's keys of a share lie in one group of 16, so in one page: eight rows
+      // of 128 bytes in e4m3, four of 256 in bf16, from key first_key(i)
+      auto first_key = [&](int i) { return kRowsWave * (W * i + wave); };
       auto fetch = [&](int s) __attribute__((always_inline)) {
         const int kb = s * kTile, valid = min(kTile, ex.ctx - kb);
         in_flight = valid == 64 ? ~0ull : (1ull << valid) - 1;
-        int pg[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          pg[i] = __builtin_amdgcn_readlane(page, i);
-          if (uint32_t(pg[i]) >= uint32_t(a.c.num_pages)) {
-            in_flight &= ~(0xFFFFull << (16 * i));
-            pg[i] = 0;   // any page: what is read is not used
-          }
-        }
+        for (int i = 0; i < 4; ++i)
+          if (uint32_t(__builtin_amdgcn_readlane(page, i)) >= uint32_t(a.c.num_pages)) in_flight &= ~(0xFFFFull << (16 * i));
 #pragma unroll
         for (int i = 0; i < kShares; ++i) {
-          const int64_t of = !E8 ? pg[i] : wave < 2 ? pg[2 * i & 3] : pg[(2 * i + 1) & 3];
-          const int64_t row0 = ((of * a.heads_kv + kvh) << a.c.page_log2) + ((kb + (E8 ? 32 * i + 8 * wave : 16 * i + 4 * wave)) & page_mask);
+          const int of = __builtin_amdgcn_readlane(page, first_key(i) >> 4);
+          const int64_t in = uint32_t(of) < uint32_t(a.c.num_pages) ? of : 0;   // any page: what is read is not used
+          const int64_t row0 = ((in * a.heads_kv + kvh) << a.c.page_log2) + ((kb + first_key(i)) & page_mask);
           const int64_t byte0 = row0 * (E8 ? kHead : 2 * kHead);
           kx[i] = *reinterpret_cast<const u32x4*>(static_cast<const char*>(a.c.k) + byte0 + 16 * lane);
           vx[i] = *reinterpret_cast<const u32x4*>(static_cast<const char*>(a.c.v) + byte0 + 16 * lane);
@@ -750,7 +746,7 @@ __global__ __launch_bounds__(256, 2) void paged_tiles(PagedArgs a, int whole) {
         LDS_AS char* const kt = lds + B.value * 2 * kTileBytes;
 #pragma unroll
         for (int i = 0; i < kShares; ++i) {
-          const int key = E8 ? 32 * i + 8 * wave + (lane >> 3) : 16 * i + 4 * wave + g;
+          const int key = first_key(i) + (E8 ? lane >> 3 : g);
           const bool gone = there != ~0ull && !((there >> key) & 1);
           if (gone) vx[i] = zero;
           if constexpr (E8) {
@@ -784,8 +780,9 @@ __global__ __launch_bounds__(256, 2) void paged_tiles(PagedArgs a, int whole) {
     }
     {   // the tree's own keys
       const int words = (a.budget + 63) / 64;
+      constexpr int kShares = kTile / (4 * W);
       const int key0 = tid >> 4, c = tid & 15;
-      u32x4 kx[4], vx[4];
+      u32x4 kx[kShares], vx[kShares];
       uint64_t in_flight = 0, next_seen[RG], seen[RG];   // mask words of the tile in flight, of the stored one
       auto fetch = [&](int s) __attribute__((always_inline)) {
         const int kb = (s - nctx) * kTile, valid = min(kTile, ex.nodes - kb);   // 0 where a request has no keys at all
@@ -796,8 +793,8 @@ __global__ __launch_bounds__(256, 2) void paged_tiles(PagedArgs a, int whole) {
             next_seen[r] = a.mask[(int64_t(q) * a.budget + node[r]) * words + min(s - nctx, words - 1)];
         }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int key = min(kb + 16 * i + key0, a.budget - 1);
+        for (int i = 0; i < kShares; ++i) {
+          const int key = min(kb + 4 * W * i + key0, a.budget - 1);
           const int64_t off = (int64_t(q) * a.budget + key) * a.kv_stride + kvh * kHead + 8 * c;
           kx[i] = *reinterpret_cast<const u32x4*>(a.k_tree + off);
           vx[i] = *reinterpret_cast<const u32x4*>(a.v_tree + off);
@@ -807,8 +804,8 @@ __global__ __launch_bounds__(256, 2) void paged_tiles(PagedArgs a, int whole) {
         const u32x4 zero{0, 0, 0, 0};
         LDS_AS char* const kt = lds + B.value * 2 * kTileBytes;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int key = 16 * i + key0;
+        for (int i = 0; i < kShares; ++i) {
+          const int key = 4 * W * i + key0;
           *reinterpret_cast<LDS_AS u32x4*>(kt + key * kRowBytes + (c ^ k_place(key)) * 16) = kx[i];
           *reinterpret_cast<LDS_AS u32x4*>(kt + kTileBytes + key * kRowBytes + (c ^ v_place(key)) * 16) =
               (in_flight >> key) & 1 ? vx[i] : zero;
@@ -933,7 +930,7 @@ __global__ __launch_bounds__(256) void paged_join(PagedArgs a, int blocks) {
 
 // Which kernel, its tile's query rows and the blocks of a launch: as many as the
 // chip holds, sharing the line of steps, or one per item.
-enum Kernel { kFew, kFewWhole, kTiles64, kTiles128 };
+enum Kernel { kFew, kFewWhole, kTiles64, kTiles128, kTiles256 };
 struct Plan {
   Kernel kernel;
   int rows, blocks, whole;
@@ -962,12 +959,16 @@ Plan plan_of(int batch, int budget, int max_ctx, int heads_q, int heads_kv, int 
   }
   const int step = rows <= 16 ? 128 : kTile;
   const int64_t steps = (int64_t(max_ctx) + step - 1) / step + (budget + step - 1) / step;
-  // 128 rows a tile double a tile's products per byte from LDS, and a cut item's
-  // partial results; worth it where blocks take eight steps and more
-  p.kernel = rows <= 16 ? kFew : rows <= 64 || tiles_of(128) * steps < 8 * kResident ? kTiles64 : kTiles128;
-  p.rows = p.kernel == kFew ? 16 : p.kernel == kTiles64 ? 64 : 128;
+  // 128 rows a tile (two groups a wave) double a tile's products per byte from LDS,
+  // and a cut item's partial results; worth it where blocks take eight steps and
+  // more.  256 rows (eight waves) halve the work of storing tiles; worth it where
+  // whole items fill the chip and few of their rows are idle (16 x 512 nodes x 2048
+  // positions, 32 / 8 heads: 371 us, with 128 rows 397, with 64 531).
+  const bool wide = tiles_of(256) >= 1024 && 10 * 256 * tiles_of(256) <= 11 * 128 * tiles_of(128);
+  p.kernel = rows <= 16 ? kFew : rows <= 64 || tiles_of(128) * steps < 8 * kResident ? kTiles64 : wide ? kTiles256 : kTiles128;
+  p.rows = p.kernel == kFew ? 16 : p.kernel == kTiles64 ? 64 : p.kernel == kTiles128 ? 128 : 256;
   p.items = tiles_of(p.rows);
-  p.whole = p.items >= 4 * kResident;
+  p.whole = p.kernel == kTiles256 || p.items >= 4 * kResident;
   p.blocks = int(p.whole ? p.items : std::min<int64_t>(kResident, p.items * steps));
   return p;
 }
@@ -997,9 +998,12 @@ hipError_t launch_paged_attention(const PagedArgs& a, hipStream_t s) {
       return a.eight ? launch<16, 256, 512>(paged_attention<1, true, 8>, a, p, s)
                      : launch<16, 256, 512>(paged_attention<1, false, 8>, a, p, s);
     case kTiles64:
-      return a.eight ? launch<64, kTile>(paged_tiles<1, true>, a, p, s) : launch<64, kTile>(paged_tiles<1, false>, a, p, s);
+      return a.eight ? launch<64, kTile>(paged_tiles<1, true, 4>, a, p, s) : launch<64, kTile>(paged_tiles<1, false, 4>, a, p, s);
+    case kTiles128:
+      return a.eight ? launch<128, kTile>(paged_tiles<2, true, 4>, a, p, s) : launch<128, kTile>(paged_tiles<2, false, 4>, a, p, s);
     default:
-      return a.eight ? launch<128, kTile>(paged_tiles<2, true>, a, p, s) : launch<128, kTile>(paged_tiles<2, false>, a, p, s);
+      return a.eight ? launch<256, kTile, 512>(paged_tiles<2, true, 8>, a, p, s)
+                     : launch<256, kTile, 512>(paged_tiles<2, false, 8>, a, p, s);
   }
 }
 

@@ -188,6 +188,18 @@ def test_many_requests(kind, b, n, ctx, hq, hkv):
 
 
 @pytest.mark.parametrize("kind", [E8, BF])
+@pytest.mark.parametrize("n,hq,chain", [(64, 32, False), (125, 16, True), (70, 32, False)])
+def test_many_large_trees(kind, n, hq, chain):
+    """256, 250 and 280 query rows a key/value head, enough of them for one block each."""
+    rng = np.random.default_rng(n)
+    lens = rng.integers(0, 200, size=128)
+    lens[5], lens[77] = 0, 199
+    c = Case(128, n, 199, hq, 8, 16, kind, lens=lens, chain=chain, num_nodes=rng.integers(1, n + 1, size=128), seed=11,
+             holes=[(77, 3, -1), (9, 0, 1 << 30)])
+    c.check(requests=[0, 5, 9, 77, 127], heads=[0, hq - 1])
+
+
+@pytest.mark.parametrize("kind", [E8, BF])
 @pytest.mark.parametrize("b,n,ctx", [(1, 1, 40000), (2, 16, 20011), (1, 64, 9000)])
 def test_long_contexts(kind, b, n, ctx):
     Case(b, n, ctx, 8, 2, 64, kind, seed=7).check(heads=[0, 7])
