@@ -12,9 +12,8 @@
 //
 // Trees: with few rows the records of every row are taken at once (one pass
 // over the logits, all compute units) and a block per request then walks the
-// tree in LDS.  With many, only the rows on the path are read, one level per
-// launch, whose last block of a request takes the step.  Chains: the records of
-// every row, then one pass over the final row.
+// tree in LDS.  With many, only rows along the likeliest paths are read (below).
+// Chains: the records of every row, then one pass over the final row.
 #include <algorithm>
 
 #include "reduce.hpp"
@@ -38,8 +37,8 @@ struct Record {
 // What blocks of one launch hand to the request's last block goes past the
 // caches of a compute unit and an XCD (relaxed atomics of the device's scope), and
 // a block arrives once its words are there.  A release and an acquire instead
-// write back and drop a whole L2: 24 us for the final token of eight chains
-// against 17.
+// write back and drop a whole L2: 24.2 us for the final tokens of eight chains
+// against 21.7.
 __device__ __forceinline__ void hand_over(uint64_t* p, uint64_t x) {
   __hip_atomic_store(p, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
@@ -49,21 +48,6 @@ __device__ __forceinline__ uint64_t taken_over(const uint64_t* p) {
 __device__ __forceinline__ bool arrive_last(int32_t* arrived, int blocks) {
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   return __hip_atomic_fetch_add(arrived, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == blocks - 1;
-}
-
-struct RecordWords {
-  uint64_t w[2];
-};
-__device__ __forceinline__ void put_record(Record* to, const Record& r) {
-  const RecordWords x = __builtin_bit_cast(RecordWords, r);
-  hand_over(reinterpret_cast<uint64_t*>(to), x.w[0]);
-  hand_over(reinterpret_cast<uint64_t*>(to) + 1, x.w[1]);
-}
-template <bool TAKEN>   // TAKEN: written in this launch
-__device__ __forceinline__ Record get_record(const Record* from) {
-  if (!TAKEN) return *from;
-  const uint64_t* p = reinterpret_cast<const uint64_t*>(from);
-  return __builtin_bit_cast(Record, RecordWords{{taken_over(p), taken_over(p + 1)}});
 }
 
 // exp(x) for x <= 0 (or -inf): 2^n 2^f with |f| <= 1/2, the Taylor series of
@@ -169,28 +153,27 @@ __device__ __forceinline__ int wave_min_int(int x) {
 }
 __device__ __forceinline__ int wave_max_int(int x) { return -wave_min_int(-x); }
 
-// A block's share of a segment in registers, and the segment's record from it.
+// A block's share of a segment in registers, and the segment's record from it
+// (table: kExp32 in LDS).
 template <bool BF, int NT>
 struct Segment {
   static constexpr int N = RowView<BF>::N, L = kSeg / N / NT;
   float x[L][N];
   int first[L];
-  __device__ Segment(const RowView<BF>& z, int seg) {
+  __device__ void load(const RowView<BF>& z, int seg) {
 #pragma unroll
     for (int l = 0; l < L; ++l) z.template load<true>(seg * (kSeg / N) + l * NT + threadIdx.x, x[l], first[l]);
   }
 };
 template <bool BF, int NT>
-__device__ __forceinline__ void segment_record(const Segment<BF, NT>& in, double c, Record* out) {
+__device__ __forceinline__ void segment_record(const Segment<BF, NT>& in, const double* table, double c, Record* out) {
   constexpr int N = RowView<BF>::N, L = kSeg / N / NT, W = NT / 64;
-  __shared__ double table[32];
   __shared__ float sm[W];
   __shared__ int sa[W];
   __shared__ double ss[W];
   const auto& x = in.x;
   const auto& first = in.first;
   float m = -INFINITY;
-  if (threadIdx.x < 32) table[threadIdx.x] = kExp32[threadIdx.x];
 #pragma unroll
   for (int l = 0; l < L; ++l)
 #pragma unroll
@@ -245,13 +228,12 @@ __device__ __forceinline__ void segment_record(const Segment<BF, NT>& in, double
       if (c == 0.0) r.arg = min(r.arg, sa[w]);
       else r.s += ss[w];
     }
-    put_record(out, r);
+    *out = r;
   }
 }
 
 // A row's records joined by 8 lanes (kJoin); the same in each.
 constexpr int kJoin = 8;
-template <bool TAKEN = false>
 __device__ __forceinline__ Record join_records(const Record* rec, int nseg, double c) {
   constexpr int H = 5;   // records at a time: 8 x 5 are those of 163840 tokens
   const int l = threadIdx.x & (kJoin - 1);
@@ -261,7 +243,7 @@ __device__ __forceinline__ Record join_records(const Record* rec, int nseg, doub
     float m = r.m;
 #pragma unroll
     for (int h = 0; h < H; ++h) {
-      o[h] = get_record<TAKEN>(rec + min(i0 + kJoin * h, nseg - 1));
+      o[h] = rec[min(i0 + kJoin * h, nseg - 1)];
       if (i0 + kJoin * h >= nseg) o[h].m = -INFINITY;
       m = fmaxf(m, o[h].m);
     }
@@ -451,7 +433,11 @@ __global__ __launch_bounds__(256) void row_records(const void* z, int64_t zrows,
     for (int i = threadIdx.x; i < ncounters; i += 256) counters[i] = 0;
   const int row = blockIdx.x / nseg, seg = blockIdx.x - row * nseg;
   const RowView<BF> v(row < zrows ? z : y, row < zrows ? row : row - zrows, stride, vocab);
-  segment_record<BF, 256>(Segment<BF, 256>(v, seg), c, rec + blockIdx.x);
+  __shared__ double table[32];
+  Segment<BF, 256> s;
+  s.load(v, seg);
+  if (threadIdx.x < 32) table[threadIdx.x] = kExp32[threadIdx.x];   // read after a barrier
+  segment_record<BF, 256>(s, table, c, rec + blockIdx.x);
 }
 
 // ---------------------------------------------------------------------------
@@ -461,7 +447,7 @@ __global__ __launch_bounds__(256) void row_records(const void* z, int64_t zrows,
 // The final token of row `row` without the tokens of `gone` (LDS; the shares of the
 // first kShares in `share`), by a block of NT threads.
 constexpr int kShares = 64;
-template <bool BF, int NT, bool TAKEN>
+template <bool BF, int NT>
 __device__ int final_token(const VerifyArgs& a, int64_t row, const Record* rec, int nseg, const Law& law, const int32_t* gone,
                            const double* share, int ngone, float u, double* segw) {
   constexpr int N = RowView<BF>::N;
@@ -472,7 +458,7 @@ __device__ int final_token(const VerifyArgs& a, int64_t row, const Record* rec, 
     const int n = pass == 0 ? ngone : 0;
     bool again = false;
     for (int s = threadIdx.x; s < nseg; s += NT) {
-      const Record r = get_record<TAKEN>(rec + s);
+      const Record r = rec[s];
       const double all = r.m == -INFINITY ? 0.0 : r.s * exp64((double(r.m) - law.m) * law.c);
       double w = all;
       bool many = false;
@@ -605,122 +591,250 @@ __global__ __launch_bounds__(kWalkNodes) void tree_walk(VerifyArgs a, int nseg, 
   __syncthreads();
   const int at = at_s;
   const Law law(Record{rm[at + 1], rarg[at + 1], rs[at + 1]}, c);
-  const int t = final_token<BF, kWalkNodes, false>(a, int64_t(q) * (B + 1) + at + 1, qrec + int64_t(at + 1) * nseg, nseg, law, tok, share, tested_s,
+  const int t = final_token<BF, kWalkNodes>(a, int64_t(q) * (B + 1) + at + 1, qrec + int64_t(at + 1) * nseg, nseg, law, tok, share, tested_s,
                                 a.uniforms[int64_t(q) * (B + 1)], segw);
   if (threadIdx.x == 0) a.bonus[q] = t;
 }
 
-constexpr int kPick = 512;   // threads of the blocks below
+// Many rows: only those on the likeliest path are read.  Per request, the drafted
+// tokens' logits give every node its best child without any row's law; the rows
+// along the best children from the current node are read in one launch, and a
+// walk goes on until it leaves them.  kRounds of that, the first with the few rows
+// that most trees end in, and the last walk reads the rows it still lacks by
+// itself (a block per request, 30 us a row): a sampled path leaves the best
+// children seldom and then ends soon.  16 trees of 512 nodes of depth 16, vocab
+// 151936 fp32: 2 rounds of 17 rows 83.9 us, of 8 and 17 88.2, a third round 78.4,
+// a fourth 82.9.  One node a launch, its last block walking on, took 194.
+constexpr int kFirstRows = 8;   // rows of the first round
+constexpr int kPathRows = 32;   // and of the others
+constexpr int kRounds = 3;
+constexpr int kPathThreads = 1024;
 
-// State of a request's walk, level by level.
 struct Walk {
-  int32_t at, count, done, arrived;   // arrived: blocks of this level whose record is written
+  int32_t at, count, done, len;   // current node, accepted nodes, rows of the path to read
+  int32_t path[kPathRows];
 };
-__global__ __launch_bounds__(256) void walk_begin(Walk* walk, int batch) {
-  const int q = blockIdx.x * 256 + threadIdx.x;
-  if (q < batch) walk[q] = Walk{-1, 0, 0, 0};
+
+// The rows from the current node along the best children (child[row]: best child
+// of the node of that row, -1: none), at most as many as can still be accepted.
+__device__ __forceinline__ void plan_path(Walk* w, int at, int count, int rows, int max_len, const int32_t* child) {
+  int len = 0, row = at + 1;
+  while (true) {
+    w->path[len++] = row;
+    if (len == rows || count + len > max_len) break;
+    const int c = child[row];
+    if (c < 0) break;
+    row = c + 1;
+  }
+  w->at = at;
+  w->count = count;
+  w->done = 0;
+  w->len = len;
 }
 
-// One level: block (request, segment) takes the record of its segment of the
-// current row, and the request's last block to arrive takes the step.
+// Block per request: the drafted tokens' logits zd [b][B], every row's best child
+// [b][B+1] (the largest logit, the lowest index among equals), the first path.
 template <bool BF>
-__global__ __launch_bounds__(kPick) void walk_level(VerifyArgs a, int nseg, double c, Walk* walk, Record* rec) {
-  __shared__ uint16_t kid[DARTREE_MAX_SORT];
-  __shared__ int32_t gone[DARTREE_MAX_SORT], tkid[kPick];   // tkid, ukid, zkid: the first kPick children
-  __shared__ float ukid[kPick], zkid[kPick];
-  __shared__ double share[kShares];
-  __shared__ int wcount[kPick / 64], next_s, ngone_s, last_s;
-  __shared__ double segw[kMaxSeg];
-  const int q = blockIdx.x / nseg, seg = blockIdx.x - q * nseg, B = a.budget;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const Walk w = walk[q];   // `arrived` changes meanwhile and is not used
-  if (w.done) return;
-  const int64_t row = int64_t(q) * (B + 1) + w.at + 1;
-  const RowView<BF> z(a.target, row, a.row_stride, a.vocab);
-  const Segment<BF, kPick> part(z, seg);
-  // the current node's children in index order, in every block while its segment
-  // arrives: the last block needs them at once
-  const int n = min(max(a.num_nodes[q], 0), B);
-  int nkid = 0;
-  if (w.count < min(a.max_len, n))
-    for (int j0 = 0; j0 < n; j0 += kPick) {
-      const int j = j0 + threadIdx.x;
-      const bool is = j < n && a.parents[int64_t(q) * B + j] == w.at;
-      const uint64_t b = __ballot(is);
-      __syncthreads();
-      if (lane == 0) wcount[wave] = __popcll(b);
-      __syncthreads();
-      int at = nkid + __popcll(b & ((1ull << lane) - 1));
-      for (int x = 0; x < kPick / 64; ++x) {
-        if (x < wave) at += wcount[x];
-        nkid += wcount[x];
-      }
-      if (is) kid[at] = uint16_t(j);
+__global__ __launch_bounds__(kPathThreads) void path_begin(VerifyArgs a, Walk* walk, float* zd, int32_t* child) {
+  __shared__ unsigned long long best[DARTREE_MAX_SORT + 1];
+  __shared__ int32_t kid[DARTREE_MAX_SORT + 1];
+  const int q = blockIdx.x, B = a.budget, n = min(max(a.num_nodes[q], 0), B);
+  for (int r = threadIdx.x; r <= n; r += kPathThreads) best[r] = 0;
+  __syncthreads();
+  for (int j = threadIdx.x; j < n; j += kPathThreads) {
+    const int t = a.tokens[int64_t(q) * B + j], p = a.parents[int64_t(q) * B + j];
+    float z = -INFINITY;
+    if (p >= -1 && p < n && t >= 0 && t < a.vocab) {
+      z = RowView<BF>(a.target, int64_t(q) * (B + 1) + p + 1, a.row_stride, a.vocab).at(t);
+      // a key is never 0, and a maximum does not depend on the order
+      atomicMax(&best[p + 1], (unsigned long long)rank_key(z, j));
     }
+    zd[int64_t(q) * B + j] = z;
+  }
   __syncthreads();
-  auto read_kid = [&](int i, int& t, float& u, float& x) {
-    t = a.tokens[int64_t(q) * B + kid[i]];
-    u = a.uniforms[int64_t(q) * (B + 1) + kid[i] + 1];
-    x = t >= 0 && t < a.vocab ? z.at(t) : -INFINITY;
-  };
-  if (int(threadIdx.x) < nkid) read_kid(threadIdx.x, tkid[threadIdx.x], ukid[threadIdx.x], zkid[threadIdx.x]);
-  segment_record<BF, kPick>(part, c, rec + blockIdx.x);
-  if (threadIdx.x == 0) last_s = arrive_last(&walk[q].arrived, nseg);   // the thread that put the record
+  for (int r = threadIdx.x; r <= n; r += kPathThreads) {
+    const int c = best[r] ? key_id(best[r]) : -1;
+    kid[r] = c == r - 1 ? -1 : c;   // not itself
+    child[int64_t(q) * (B + 1) + r] = kid[r];
+  }
   __syncthreads();
-  if (!last_s) return;
-  const Law law(join_records<true>(rec + int64_t(q) * nseg, nseg, c), c);
-  if (wave == 0) {
-    double taken = 0.0;
-    int next = -1, m = 0;
-    for (int i0 = 0; i0 < nkid && next < 0; i0 += 64) {
-      const int i = i0 + lane;
-      int t = -1;
-      float u = 0.f, x = -INFINITY;
-      if (i < min(nkid, kPick)) t = tkid[i], u = ukid[i], x = zkid[i];
-      else if (i < nkid) read_kid(i, t, u, x);
-      const bool in = t >= 0 && t < a.vocab;
-      const double s = in ? law.share(x, t) : 0.0;
+  if (threadIdx.x == 0) plan_path(walk + q, -1, 0, kFirstRows, min(a.max_len, n), kid);
+}
+
+// The records of the paths' rows: block (request, row of its path, segment).
+template <bool BF>
+__global__ __launch_bounds__(256) void path_records(VerifyArgs a, int nseg, int rows, int nrows, double c, const Walk* walk, Record* rec) {
+  __shared__ double table[32];
+  const int seg = blockIdx.x % nseg, i = blockIdx.x / nseg % rows, q = blockIdx.x / nseg / rows;
+  if (walk[q].done || i >= walk[q].len) return;
+  if (threadIdx.x < 32) table[threadIdx.x] = kExp32[threadIdx.x];   // read after a barrier
+  const RowView<BF> z(a.target, int64_t(q) * (a.budget + 1) + walk[q].path[i], a.row_stride, a.vocab);
+  Segment<BF, 256> s;
+  s.load(z, seg);
+  segment_record<BF, 256>(s, table, c, rec + (int64_t(q) * nrows + i) * nseg + seg);
+}
+
+// A segment's record by one wave.
+template <bool BF>
+__device__ __forceinline__ void wave_record(const RowView<BF>& z, int seg, const double* table, double c, Record* out) {
+  constexpr int N = RowView<BF>::N, L = kSeg / N / 64;
+  float m = -INFINITY;
+  for (int l = 0; l < L; ++l) {
+    float x[N];
+    int first;
+    z.load(seg * (kSeg / N) + l * 64 + (threadIdx.x & 63), x, first);
+#pragma unroll
+    for (int i = 0; i < N; ++i) m = fmaxf(m, x[i]);
+  }
+  m = wave_max(m);
+  int arg = INT32_MAX;
+  double s = 0.0;
+  const ExpTable e(table, c, m);
+  if (m != -INFINITY)
+    for (int l = 0; l < L; ++l) {
+      float x[N];
+      int first;
+      z.load(seg * (kSeg / N) + l * 64 + (threadIdx.x & 63), x, first);
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        if (c == 0.0) arg = x[i] == m ? min(arg, first + i) : arg;
+        else e.add(x[i], s);
+      }
+    }
+  if (c == 0.0) arg = wave_min_int(arg);
+  else s = wave_sum64(s);
+  if ((threadIdx.x & 63) == 0) *out = Record{m, c == 0.0 ? arg : 0, s};
+}
+
+// The first child of `at` whose token is taken, -1: none (one wave).  FILL: the
+// children's tokens and shares are gathered, m of them.
+template <bool FILL>
+__device__ __forceinline__ int test_children(const Law& law, int at, int n, int vocab, const int32_t* tok, const int32_t* par,
+                                             const float* us, const float* zs, int32_t* gone, double* share, int& m) {
+  const int lane = threadIdx.x & 63;
+  double taken = 0.0;
+  for (int j0 = 0; j0 < n; j0 += 64) {
+    const int j = j0 + lane;
+    const bool is = j < n && par[j] == at;
+    uint64_t kids = __ballot(is);
+    if (!kids) continue;
+    const int t = is ? tok[j] : -1;
+    const bool in = t >= 0 && t < vocab;
+    const double s = in ? law.share(zs[j], t) : 0.0;
+    if (FILL) {
       const uint64_t b = __ballot(in);
-      const int at = m + __popcll(b & ((1ull << lane) - 1));
-      if (in) gone[at] = t;
-      if (in && at < kShares) share[at] = s;
+      const int to = m + __popcll(b & ((1ull << lane) - 1));
+      if (in) gone[to] = t;
+      if (in && to < kShares) share[to] = s;
       m += __popcll(b);
-      for (int x0 = 0; x0 < min(64, nkid - i0); ++x0) {
-        const double si = __shfl(s, x0);
-        if (double(__shfl(u, x0)) * (1.0 - taken) < si) {
-          next = i0 + x0;
-          break;
-        }
-        taken += si;
+      continue;
+    }
+    const float u = is ? us[j] : 0.f;
+    while (kids) {
+      const int l = __builtin_ctzll(kids);
+      kids &= kids - 1;
+      const double sl = __shfl(s, l);
+      if (double(__shfl(u, l)) * (1.0 - taken) < sl) return j0 + l;
+      taken += sl;
+    }
+  }
+  return -1;
+}
+
+// Block per request: walk as far as the path's rows reach, LAST: to the end.  The
+// children of all rows on the path are tested at once, a wave per row; the walk is
+// then a few steps in LDS (16 trees of 512 nodes: 15 us; one wave that goes from
+// node to node takes 26).
+template <bool BF, bool LAST>
+__global__ __launch_bounds__(kPathThreads) void path_walk(VerifyArgs a, int nseg, int nrows, double c, Walk* walk, Record* rec,
+                                                          const float* zd, const int32_t* child) {
+  __shared__ int32_t tok[DARTREE_MAX_SORT], par[DARTREE_MAX_SORT], kid[DARTREE_MAX_SORT + 1], gone[DARTREE_MAX_SORT];
+  __shared__ float us[DARTREE_MAX_SORT], zs[DARTREE_MAX_SORT];
+  __shared__ float rm[kPathRows];
+  __shared__ int32_t rarg[kPathRows], path[kPathRows], next[kPathRows];
+  __shared__ double rs[kPathRows], share[kShares], table[32], segw[kMaxSeg];
+  __shared__ int ngone;
+  const int q = blockIdx.x, B = a.budget, wave = threadIdx.x >> 6;
+  Walk& w = walk[q];
+  if (w.done) return;
+  const int n = min(max(a.num_nodes[q], 0), B);
+  Record* qrec = rec + int64_t(q) * nrows * nseg;
+  int len = w.len, at = w.at, count = w.count;
+  for (int i = threadIdx.x; i < len; i += kPathThreads) path[i] = w.path[i];
+  for (int j = threadIdx.x; j < n; j += kPathThreads) {
+    tok[j] = a.tokens[int64_t(q) * B + j];
+    par[j] = a.parents[int64_t(q) * B + j];
+    us[j] = a.uniforms[int64_t(q) * (B + 1) + j + 1];
+    zs[j] = zd[int64_t(q) * B + j];
+  }
+  if (!LAST)
+    for (int r = threadIdx.x; r <= n; r += kPathThreads) kid[r] = child[int64_t(q) * (B + 1) + r];
+  if (threadIdx.x < 32) table[threadIdx.x] = kExp32[threadIdx.x];
+  const int steps = min(a.max_len, n);
+  int slot, m = 0;
+  while (true) {   // once, and again for each row that LAST reads; a turn accepts a node or ends
+    for (int i = threadIdx.x / kJoin; i < len; i += kPathThreads / kJoin) {
+      const Record r = join_records(qrec + int64_t(i) * nseg, nseg, c);
+      if (threadIdx.x % kJoin == 0) {
+        rm[i] = r.m;
+        rarg[i] = r.arg;
+        rs[i] = r.s;
       }
     }
-    if (lane == 0) {
-      next_s = next < 0 ? -1 : kid[next];
-      ngone_s = m;
+    __syncthreads();
+    for (int i = wave; i < len; i += kPathThreads / 64) {
+      int none = 0;
+      const int j = count + i < steps
+                        ? test_children<false>(Law(Record{rm[i], rarg[i], rs[i]}, c), path[i] - 1, n, a.vocab, tok, par, us, zs, gone, share, none)
+                        : -1;
+      if ((threadIdx.x & 63) == 0) next[i] = j;
     }
+    __syncthreads();
+    // the same by every thread
+    for (slot = 0;;) {
+      const int j = next[slot];
+      if (j < 0) break;
+      if (threadIdx.x == 0) a.accepted[int64_t(q) * a.max_len + count] = j;
+      at = j;
+      ++count;
+      if (slot + 1 == len || path[slot + 1] != at + 1) {
+        slot = -1;   // off the path
+        break;
+      }
+      ++slot;
+    }
+    if (slot >= 0) break;
+    if (!LAST) {
+      if (threadIdx.x == 0) plan_path(&w, at, count, kPathRows, steps, kid);
+      return;
+    }
+    const RowView<BF> z(a.target, int64_t(q) * (B + 1) + at + 1, a.row_stride, a.vocab);
+    for (int s = wave; s < nseg; s += kPathThreads / 64) wave_record<BF>(z, s, table, c, qrec + s);
+    __syncthreads();
+    if (threadIdx.x == 0) path[0] = at + 1;
+    len = 1;
   }
+  const Law law(Record{rm[slot], rarg[slot], rs[slot]}, c);
+  if (wave == 0) {
+    if (count < steps) test_children<true>(law, at, n, a.vocab, tok, par, us, zs, gone, share, m);
+    if (threadIdx.x == 0) ngone = m;
+  }
+  for (int j = count + threadIdx.x; j < a.max_len; j += kPathThreads) a.accepted[int64_t(q) * a.max_len + j] = -1;
   __syncthreads();
-  const int next = next_s;
-  if (next >= 0) {
-    if (threadIdx.x == 0) {
-      a.accepted[int64_t(q) * a.max_len + w.count] = next;
-      walk[q] = Walk{next, w.count + 1, 0, 0};
-    }
-    return;
-  }
-  for (int j = w.count + threadIdx.x; j < a.max_len; j += kPick) a.accepted[int64_t(q) * a.max_len + j] = -1;
-  const int t = final_token<BF, kPick, true>(a, row, rec + int64_t(q) * nseg, nseg, law, gone, share, ngone_s,
-                                a.uniforms[int64_t(q) * (B + 1)], segw);
+  const int t = final_token<BF, kPathThreads>(a, int64_t(q) * (B + 1) + at + 1, qrec + int64_t(slot) * nseg, nseg, law, gone, share,
+                                              ngone, a.uniforms[int64_t(q) * (B + 1)], segw);
   if (threadIdx.x == 0) {
-    a.num_accepted[q] = w.count;
+    a.num_accepted[q] = count;
     a.bonus[q] = t;
-    walk[q] = Walk{w.at, w.count, 1, 0};
+    w.done = 1;
   }
 }
 
 // ---------------------------------------------------------------------------
 // Chains
 // ---------------------------------------------------------------------------
+
+constexpr int kPick = 512;   // threads of the blocks below
 
 // Laws of the rows of a request's chain in LDS, and how many tokens pass.
 struct ChainRows {
@@ -862,15 +976,37 @@ __global__ __launch_bounds__(kPick) void chain_final(VerifyArgs a, int nseg, dou
 constexpr size_t kAlign = 256;
 size_t up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
 
-// All rows at once or level by level.
-bool by_level(int, int budget, int, int) { return budget > 256; }
+// Rows of a request's path in a round, and whether to go by paths: that is worth
+// its launches once it leaves 64 MB of logits unread (counted as fp32: the
+// workspace is sized without the type).  Every row / by paths, us, path_rows 17:
+//   batch 1, 64 nodes, vocab 151936, 29 MB unread    24.3 / 26.6
+//   batch 16, 64 nodes, vocab 32000, 98 MB           45.3 / 43.6
+//   batch 4, 64 nodes, vocab 151936, 117 MB          54.5 / 45.3
+//   batch 1, 512 nodes, vocab 151936, 301 MB         93.9 / 26.2
+//   batch 16, 512 nodes, vocab 151936, 4.8 GB        1200 / 78.4
+int path_rows(int budget, int max_len) { return std::min({kPathRows, max_len + 1, budget + 1}); }
+bool by_path(int batch, int budget, int max_len, int vocab) {
+  return budget > kWalkNodes || 4.0 * vocab * batch * (budget + 1 - path_rows(budget, max_len)) > 64e6;
+}
+struct PathLayout {
+  size_t walk, zd, child, rec, total;
+};
+PathLayout path_layout(int batch, int budget, int max_len, int vocab) {
+  const size_t b = batch, B = budget;
+  PathLayout l{};
+  l.zd = up(b * sizeof(Walk));
+  l.child = l.zd + up(b * B * sizeof(float));
+  l.rec = l.child + up(b * (B + 1) * sizeof(int32_t));
+  l.total = l.rec + up(b * path_rows(budget, max_len) * segments(vocab) * sizeof(Record));
+  return l;
+}
 
 template <bool BF>
 hipError_t tree(const VerifyArgs& a, hipStream_t s) {
   const int nseg = segments(a.vocab);
   const double c = a.inv_t * 1.4426950408889634;
   hipError_t e;
-  if (!by_level(a.batch, a.budget, a.max_len, a.vocab)) {
+  if (!by_path(a.batch, a.budget, a.max_len, a.vocab)) {
     Record* rec = static_cast<Record*>(a.ws);
     const int64_t rows = int64_t(a.batch) * (a.budget + 1);
     hipLaunchKernelGGL(row_records<BF>, dim3(unsigned(rows * nseg)), dim3(256), 0, s, a.target, rows, nullptr, a.row_stride,
@@ -879,12 +1015,23 @@ hipError_t tree(const VerifyArgs& a, hipStream_t s) {
     hipLaunchKernelGGL(tree_walk<BF>, dim3(a.batch), dim3(kWalkNodes), 0, s, a, nseg, c, rec);
     return hipGetLastError();
   }
-  Walk* walk = static_cast<Walk*>(a.ws);
-  Record* rec = reinterpret_cast<Record*>(static_cast<char*>(a.ws) + up(a.batch * sizeof(Walk)));
-  hipLaunchKernelGGL(walk_begin, dim3((a.batch + 255) / 256), dim3(256), 0, s, walk, a.batch);
+  const PathLayout l = path_layout(a.batch, a.budget, a.max_len, a.vocab);
+  const int nrows = path_rows(a.budget, a.max_len);
+  char* ws = static_cast<char*>(a.ws);
+  Walk* walk = reinterpret_cast<Walk*>(ws);
+  float* zd = reinterpret_cast<float*>(ws + l.zd);
+  int32_t* child = reinterpret_cast<int32_t*>(ws + l.child);
+  Record* rec = reinterpret_cast<Record*>(ws + l.rec);
+  hipLaunchKernelGGL(path_begin<BF>, dim3(a.batch), dim3(kPathThreads), 0, s, a, walk, zd, child);
   if ((e = hipGetLastError()) != hipSuccess) return e;
-  for (int level = 0; level <= std::min(a.max_len, a.budget); ++level) {
-    hipLaunchKernelGGL(walk_level<BF>, dim3(unsigned(a.batch * nseg)), dim3(kPick), 0, s, a, nseg, c, walk, rec);
+  for (int round = 0; round < kRounds; ++round) {
+    const int rows = round ? nrows : std::min(nrows, kFirstRows);
+    hipLaunchKernelGGL(path_records<BF>, dim3(unsigned(a.batch * rows * nseg)), dim3(256), 0, s, a, nseg, rows, nrows, c, walk, rec);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+    if (round + 1 < kRounds)
+      hipLaunchKernelGGL((path_walk<BF, false>), dim3(a.batch), dim3(kPathThreads), 0, s, a, nseg, nrows, c, walk, rec, zd, child);
+    else
+      hipLaunchKernelGGL((path_walk<BF, true>), dim3(a.batch), dim3(kPathThreads), 0, s, a, nseg, nrows, c, walk, rec, zd, child);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
   return hipSuccess;
@@ -911,7 +1058,7 @@ hipError_t chain(const VerifyArgs& a, hipStream_t s) {
 
 size_t verify_tree_workspace(int batch, int budget, int max_len, int vocab) {
   const size_t nseg = segments(vocab);
-  if (by_level(batch, budget, max_len, vocab)) return up(batch * sizeof(Walk)) + up(batch * nseg * sizeof(Record));
+  if (by_path(batch, budget, max_len, vocab)) return path_layout(batch, budget, max_len, vocab).total;
   return up(size_t(batch) * (budget + 1) * nseg * sizeof(Record));
 }
 

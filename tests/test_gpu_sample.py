@@ -1,6 +1,6 @@
 """Verification from given random numbers on the GPU: the same tokens as the
 plain forms in 64 bits.  Both evaluate the definition in 64 bits, so a result
-could differ only where a random number lies within about 1e-15 of a border."""
+could differ only where a random number lies within about 1e-11 of a border."""
 import numpy as np
 import pytest
 import torch
@@ -114,6 +114,42 @@ def test_large_budgets(budget):
         check_tree(tokens, parents, np.array([budget, budget - 7]), z, 1.0, u, 12)
 
 
+def test_largest_budget_with_many_children():
+    """4096 nodes, 600 of them children of the root; every child's token is taken or every one fails."""
+    rng = np.random.default_rng(4096)
+    tokens, parents = random_trees(rng, 2, 4096, 700, spine=0.02, kids=600)
+    parents[0, :600], tokens[0, :600] = -1, rng.permutation(700)[:600]
+    z = logits_of(rng, (2, 4097, 700))
+    for first in (0.3, LAST):
+        u = rng.random((2, 4097)).astype(np.float32)
+        u[0, 1:601] = first
+        check_tree(tokens, parents, np.array([4096, 4089]), z, 1.0, u, 12)
+
+
+@pytest.mark.parametrize("held", [F32, B16])
+@pytest.mark.parametrize("temperature,keep", [(1.0, 0.8), (1.0, 0.3), (0.7, 0.05), (0.0, 0.6)])
+def test_long_paths_over_many_rows(held, temperature, keep):
+    """Enough logits that only rows on the likeliest paths are read; paths of up to 60 nodes (more than
+    a round's rows), and trees whose sampled path leaves the best children again and again."""
+    rng = np.random.default_rng(int(1000 * keep))
+    b, n, vocab = 6, 900, 9000
+    tokens, parents = random_trees(rng, b, n, vocab, spine=0.9 if keep > 0.5 else 0.3, kids=5)
+    parents[0, :60] = np.arange(-1, 59)                  # a chain of 60 at the root
+    z = boosted(logits_of(rng, (b, n + 1, vocab)), tokens, parents, rng, temperature, keep)
+    if keep < 0.5:                                       # children of equal mass: any of them may follow
+        for q in range(b):
+            for j in range(n):
+                z[q, parents[q, j] + 1, tokens[q, j]] = np.log(vocab) + 2.0
+    else:
+        z[0, np.arange(60), tokens[0, :60]] = 40.0       # sure to be followed
+    if held == B16:
+        z = S.bf16(z)
+    for max_len in (64, 3):
+        u = rng.random((b, n + 1)).astype(np.float32)
+        cnt = check_tree(tokens, parents, np.array([n, n, 5, 0, n, 700]), z, temperature, u, max_len, held)
+        assert keep < 0.5 or cnt[0] >= min(60, max_len) or temperature == 0.7
+
+
 def test_tree_edges():
     """Ends of the random numbers, rows without mass, infinities and NaN, foreign tokens and counts."""
     rng = np.random.default_rng(11)
@@ -139,6 +175,33 @@ def test_tree_edges():
     u[:, 0] = [0.0, LAST] * 5
     check_tree(tokens, parents, num, z, 1e-3, u, 8)
     check_tree(tokens, parents, num, z, 1e30, u, 8)
+
+
+def test_tree_edges_along_paths():
+    """The same in a budget whose rows are read along paths; parents in any order, also in circles."""
+    rng = np.random.default_rng(14)
+    vocab, n, budget = 300, 8, 1025
+    tokens, parents = rng.integers(0, vocab, (12, budget)), np.full((12, budget), -1)
+    tokens[:, :n], parents[:, :n] = [7, 9, 250, 3, 0, 299, 5, 6], [-1, -1, -1, 0, 0, 3, 5, 6]
+    z = logits_of(rng, (12, budget + 1, vocab))
+    z[:, 0, 7] += 8.0
+    z[:, 1, 3] += 8.0
+    u = rng.random((12, budget + 1)).astype(np.float32)
+    u[0], u[1] = 0.0, LAST
+    z[2, 0], z[3, 1] = -np.inf, -np.inf
+    u[3, 1] = 0.0
+    z[4, 0, 5:290] = np.nan
+    z[5, 0, 10] = np.inf
+    z[6, 0], z[6, 0, [7, 9, 250]] = -np.inf, 0.0
+    tokens[7, :3] = [-1, vocab, 2 ** 31 - 1]
+    parents[8, 0] = 100
+    parents[9, :n] = [3, 0, 1, -1, 3, 4, 7, 6]           # later parents, and a circle of 6 and 7
+    parents[10] = rng.integers(-3, budget + 3, budget)   # circles that the root may reach or not
+    parents[10, :3], z[10, 0, tokens[10, 0]] = -1, 9.0
+    num = np.array([8, 8, 8, 8, 8, 8, 8, 8, 8, 8, budget, 1])
+    for temperature in (1.0, 0.0, 1e-3, 1e30):
+        check_tree(tokens, parents, num, z, temperature, u, 8)
+    check_tree(tokens, parents, np.full(12, -5), z, 1.0, u, 8)
 
 
 def test_tree_little_mass_left():
