@@ -578,7 +578,10 @@ def _place(stream):
     if stream is None:
         s = torch.cuda.current_stream()
         return s.device_index, s.cuda_stream
-    return torch.cuda.current_device(), getattr(stream, "cuda_stream", stream)
+    device = torch.cuda.current_device()
+    if getattr(stream, "device_index", device) != device:
+        raise ValueError("the stream is not one of the current device")
+    return device, getattr(stream, "cuda_stream", stream)
 
 
 def _refuse(where: str, name: str, t, dtypes: tuple, shape: tuple, device: int):
