@@ -4,7 +4,8 @@
  * tree of drafted tokens over it, and the verification of drafted tokens from
  * given random numbers.  Conventions (stream, errors, alignment, validation
  * before anything is enqueued) are those of dartree.h; the calls here
- * allocate nothing and can be captured into a graph.
+ * allocate nothing and can be captured into a graph.  Sizes that would need a
+ * launch of 2^32 threads are DARTREE_ERR_UNSUPPORTED.
  *
  * A verification step of a serving loop:
  *   dartree_build_tree            the draft
@@ -69,6 +70,7 @@ dartree_status dartree_cache_validate(const dartree_cache_params* p);
  * e >= -100 for which the row's largest magnitude is at most 448 * 2^e (e =
  * -100 for a row of zeros); exp = e + 127.  Only values below 2^-15 of the
  * row's largest fall into e4m3's subnormals.
+ * A NaN stays one; an infinity becomes one, and the other values of its row 0.
  *
  * Within a call, no two (request, position) pairs may share a slot.  Slots
  * that are not written keep their contents. */
@@ -97,7 +99,9 @@ dartree_status dartree_tree_attention_paged_workspace_size(const dartree_attn_pa
  * max_ctx; values are taken into 0 .. max_ctx) and to the nodes j < num_nodes[q]
  * (NULL: budget) whose bit is set in mask row i; mask NULL: j <= i, a chain
  * (budget 1: a single token).  Positions without a page and nodes at and past
- * num_nodes[q] are not seen, and what their memory holds does not matter.
+ * num_nodes[q] are not seen, and what their memory holds does not matter; the
+ * values of the nodes below it must be finite also for rows that do not see them
+ * (their weight there is 0, and 0 times a NaN is a NaN).
  * Every row i < budget is computed; one that sees nothing is 0.
  * a: as in dartree_tree_attention, with max_ctx <= max_pages * page, batch,
  * heads_kv and head_dim as in p; max_ctx is not limited otherwise.
@@ -143,8 +147,9 @@ dartree_status dartree_verify_chain_workspace_size(int32_t batch, int32_t depth,
  * from p.  A token outside [0, vocab) has no mass.  Writes accepted
  * [b][max_len] (-1 after the last), num_accepted [b] and bonus [b] as
  * dartree_accept_walk does.  Children of one node must hold distinct tokens
- * (the builds' do; otherwise the final token is some token of the row).  1 <= budget <= DARTREE_MAX_SORT.
- * ws: device, 256-byte aligned. */
+ * (the builds' do; otherwise the final token is some token of the row).
+ * 1 <= budget <= DARTREE_MAX_SORT, 1 <= max_len <= 2^20.  ws: device, 256-byte
+ * aligned. */
 dartree_status dartree_verify_tree(int32_t batch, int32_t budget, int32_t max_len, int32_t vocab, int32_t logits_type,
                                    const int32_t* tokens, const int32_t* parents, const int32_t* num_nodes,
                                    const void* target_logits, int64_t row_stride, float temperature,

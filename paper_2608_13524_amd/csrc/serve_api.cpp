@@ -42,10 +42,10 @@ CacheView view_of(const dartree_cache_params& p, const dartree_cache& c) {
   return CacheView{p.batch, p.heads_kv, log2, p.num_pages, p.max_pages, c.k, c.v, c.k_exp, c.v_exp, c.table};
 }
 
-// Rows of 16 lanes are counted in 31 bits.
+// A launch holds fewer than 2^32 threads: rows of 16 lanes here.
 dartree_status check_rows(const dartree_cache_params& p, int32_t rows) {
   if (rows < 1) return DARTREE_ERR_INVALID_ARG;
-  if (double(p.batch) * rows * p.heads_kv > double(1 << 30)) return DARTREE_ERR_UNSUPPORTED;
+  if (double(p.batch) * rows * p.heads_kv > double(1 << 27)) return DARTREE_ERR_UNSUPPORTED;
   return DARTREE_OK;
 }
 
@@ -58,32 +58,36 @@ dartree_status check_paged(const dartree_attn_params* a, const dartree_cache_par
   if (a->batch < 1 || a->budget < 1 || a->max_ctx < 0 || a->heads_q < 1 || a->heads_kv < 1 || a->head_dim < 1)
     return DARTREE_ERR_INVALID_ARG;
   if (a->batch != p->batch || a->heads_kv != p->heads_kv || a->head_dim != p->head_dim) return DARTREE_ERR_INVALID_ARG;
-  if (a->heads_q % a->heads_kv != 0 || !isfinite(a->scale) || a->scale <= 0.f) return DARTREE_ERR_INVALID_ARG;
+  if (a->heads_q % a->heads_kv != 0 || !(a->scale > 0.f) || !isnormal(a->scale * 1.4426950408889634f))
+    return DARTREE_ERR_INVALID_ARG;
   if (a->max_ctx > int64_t(p->max_pages) * p->page) return DARTREE_ERR_INVALID_ARG;
   if (a->budget > DARTREE_MAX_SORT) return DARTREE_ERR_UNSUPPORTED;
   // items and steps are counted in 31 bits: query rows, and key steps of 128 over all requests
   if (int64_t(a->batch) * a->budget * a->heads_q > (int64_t(1) << 30)) return DARTREE_ERR_UNSUPPORTED;
+  // and a launch holds fewer than 2^32 threads: at most 512 for 16 query rows
+  if (double(a->batch) * a->heads_kv * ((int64_t(a->budget) * (a->heads_q / a->heads_kv) + 15) / 16) > double(1 << 22))
+    return DARTREE_ERR_UNSUPPORTED;
   if (int64_t(a->batch) * (a->max_ctx / 128 + a->budget / 128 + 2) > (int64_t(1) << 30)) return DARTREE_ERR_UNSUPPORTED;
   return DARTREE_OK;
 }
 
-dartree_status check_verify(int32_t batch, int32_t budget, int32_t vocab, int32_t type, float t) {
+dartree_status check_verify(int32_t batch, int32_t budget, int32_t rows, int32_t vocab, int32_t type, float t) {
   if (batch < 1 || budget < 1 || vocab < 1) return DARTREE_ERR_INVALID_ARG;
   if (type != DARTREE_FP32 && type != DARTREE_BF16) return DARTREE_ERR_INVALID_ARG;
   if (!isfinite(t) || t < 0.f) return DARTREE_ERR_INVALID_ARG;
   if (vocab > DARTREE_MAX_VOCAB) return DARTREE_ERR_UNSUPPORTED;
-  // (row, segment) blocks are counted in 31 bits
-  if (2.0 * batch * (budget + 1.0) * (vocab / 4096 + 2) > double(1 << 30) || batch > 65535) return DARTREE_ERR_UNSUPPORTED;
+  // a launch holds fewer than 2^32 threads: 256 for every segment of a request's rows
+  if (double(batch) * rows * (vocab / 4096 + 2) > double((1 << 24) - 1) || batch > 65535) return DARTREE_ERR_UNSUPPORTED;
   return DARTREE_OK;
 }
 dartree_status check_tree(int32_t batch, int32_t budget, int32_t max_len, int32_t vocab, int32_t type, float t) {
   if (max_len < 1) return DARTREE_ERR_INVALID_ARG;
-  if (budget > DARTREE_MAX_SORT) return DARTREE_ERR_UNSUPPORTED;
-  return check_verify(batch, budget, vocab, type, t);
+  if (budget > DARTREE_MAX_SORT || max_len > (1 << 20)) return DARTREE_ERR_UNSUPPORTED;
+  return check_verify(batch, budget, budget + 1, vocab, type, t);
 }
 dartree_status check_chain(int32_t batch, int32_t depth, int32_t vocab, int32_t type, float t) {
   if (depth > DARTREE_MAX_DEPTH) return DARTREE_ERR_UNSUPPORTED;
-  return check_verify(batch, depth, vocab, type, t);
+  return check_verify(batch, depth, 2 * depth + 1, vocab, type, t);
 }
 
 }  // namespace

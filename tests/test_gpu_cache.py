@@ -175,6 +175,28 @@ def test_read_back(kind, b, rows, heads, page):
         assert np.array_equal(got.float().cpu().numpy().astype(np.float64), want)
 
 
+@pytest.mark.parametrize("kind", [E8, BF])
+def test_values_that_are_not_finite(kind):
+    """bf16 keeps them; e4m3 keeps NaN, an infinity becomes NaN and its row's other values 0."""
+    dev = device()
+    p = D.CacheParams(1, 1, 128, 16, 2, 1, kind)
+    c = make_cache(p, np.array([[1]]))
+    x = torch.ones(1, 4, 1, 128, dtype=torch.bfloat16, device=dev)
+    x[0, 0, 0, 3], x[0, 1, 0, 4], x[0, 2, 0, 5], x[0, 3] = float("inf"), float("nan"), -float("inf"), float("nan")
+    say(f"cache_write of infinities and NaN type={kind}")
+    D.cache_write(p, c, x, x, 4)
+    out = [torch.zeros_like(x) for _ in range(2)]
+    D.cache_read(p, c, *out)
+    torch.cuda.synchronize()
+    want = x.float().cpu().numpy()[0, :, 0]
+    if kind == E8:
+        for row, at in ((0, 3), (2, 5)):
+            want[row] = 0.0
+            want[row, at] = np.nan
+    for o in out:
+        assert np.array_equal(o.float().cpu().numpy()[0, :, 0], want, equal_nan=True)
+
+
 def test_read_without_counts_and_past_the_table():
     rng = np.random.default_rng(3)
     p = D.CacheParams(2, 2, 128, 16, 8, 2, BF)

@@ -128,6 +128,26 @@ def test_verification_refuses_before_any_launch():
     assert chain(ws=FAKE + 16) == D.ERR_WORKSPACE
 
 
+def test_sizes_past_a_launch_are_refused():
+    """Launches of 2^32 threads and more, path lengths past 2^20, and scales whose product with log2(e) is no normal number."""
+    lib, p, c = D.lib(), cache_params(batch=64, heads_kv=64), D.CacheC(FAKE, FAKE, FAKE, FAKE, FAKE)
+    rows = (1 << 27) // (64 * 64) + 1
+    assert lib.dartree_cache_read(byref(p), byref(c), rows, FAKE, FAKE, None, None, None) == D.ERR_UNSUPPORTED
+    assert lib.dartree_cache_write(byref(p), byref(c), rows, rows, FAKE, FAKE, 8192, None, None, None, None) == D.ERR_UNSUPPORTED
+    many = cache_params(batch=1 << 16, heads_kv=128)
+    size = lambda a, p: lib.dartree_tree_attention_paged_workspace_size(byref(a), byref(p), byref(ctypes.c_size_t()))
+    assert size(D.AttnParams(1 << 16, 1, 16, 128, 128, 128, 0.1), many) == D.ERR_UNSUPPORTED
+    few = cache_params(batch=1, heads_kv=1)
+    assert size(D.AttnParams(1, 1, 16, 1, 1, 128, 0.1), few) == D.OK
+    for scale in (1e-45, 3e38, math.inf, -0.1):
+        assert size(D.AttnParams(1, 1, 16, 1, 1, 128, scale), few) == D.ERR_INVALID_ARG
+    n = ctypes.c_size_t()
+    tree = lambda *a: lib.dartree_verify_tree_workspace_size(*a, byref(n))
+    assert tree(16, 512, 2 ** 31 - 1, 151936) == D.ERR_UNSUPPORTED and tree(16, 512, (1 << 20) + 1, 151936) == D.ERR_UNSUPPORTED
+    assert tree(16, 512, 1 << 20, 151936) == D.OK and tree(4096, 512, 16, 151936) == D.ERR_UNSUPPORTED
+    assert lib.dartree_verify_chain_workspace_size(8192, 64, 151936, byref(n)) == D.ERR_UNSUPPORTED
+
+
 def test_binding_names_what_does_not_fit(monkeypatch):
     """Shapes, types and strides that the C call cannot see."""
     monkeypatch.setattr(torch.cuda, "is_initialized", lambda: False)   # before the GPU has been used
