@@ -142,13 +142,12 @@ __device__ __forceinline__ bool place_of(const PagedArgs& a, int whole, int per,
   return true;
 }
 
-template <int RG>
 struct Rows {   // a wave's running result for its query rows
-  f32x4 o[RG][8];   // o[.][t][i]: dim 32 g + 8 i + t
-  float m[RG], l[RG];   // l: this lane's keys only
+  f32x4 o[8];   // o[t][i]: dim 32 g + 8 i + t
+  float m, l;   // l: this lane's keys only
 };
 
-template <int RG, bool E8>
+template <bool E8>
 struct Chunk {   // 32 keys and values as read
   u32x4 k[2][E8 ? 2 : 4];
   u32x2 v8[E8 ? 8 : 1];
@@ -158,12 +157,11 @@ struct Chunk {   // 32 keys and values as read
 };
 
 // Scores of a chunk.
-template <int RG, bool E8>
-__device__ __forceinline__ void chunk_scores(const Chunk<RG, E8>& c, const u32x4 (&qf)[RG][4], f32x4 (&s)[RG][2]) {
+template <bool E8>
+__device__ __forceinline__ void chunk_scores(const Chunk<E8>& c, const u32x4 (&qf)[4], f32x4 (&s)[2]) {
 #pragma unroll
   for (int t = 0; t < 2; ++t) {
-#pragma unroll
-    for (int r = 0; r < RG; ++r) s[r][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    s[t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int ks = 0; ks < 4; ++ks) {
       u32x4 kf;
@@ -174,64 +172,56 @@ __device__ __forceinline__ void chunk_scores(const Chunk<RG, E8>& c, const u32x4
       } else {
         kf = c.k[t][ks];
       }
-#pragma unroll
-      for (int r = 0; r < RG; ++r) s[r][t] = mfma16(kf, qf[r][ks], s[r][t]);
+      s[t] = mfma16(kf, qf[ks], s[t]);
     }
   }
 }
 
-// Weights of a chunk from its scores.  vis: bit k set where row group r's query sees
+// Weights of a chunk from its scores.  vis: bit k set where the lane's query sees
 // key k (masked: some bit is clear).
-template <int RG>
-__device__ __forceinline__ void chunk_weights(f32x4 (&s)[RG][2], const bool masked, const uint32_t (&vis)[RG], const float c2,
-                                              Rows<RG>& st, u32x4 (&p)[RG]) {
+__device__ __forceinline__ void chunk_weights(f32x4 (&s)[2], const bool masked, const uint32_t vis, const float c2,
+                                              Rows& st, u32x4& p) {
   const int g = (threadIdx.x & 63) >> 4;
   if (masked) {
+    const uint32_t b = vis >> (4 * g);
 #pragma unroll
-    for (int r = 0; r < RG; ++r) {
-      const uint32_t b = vis[r] >> (4 * g);
+    for (int t = 0; t < 2; ++t)
 #pragma unroll
-      for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (!((b >> (16 * t + i)) & 1u)) s[r][t][i] = -INFINITY;
-    }
+      for (int i = 0; i < 4; ++i)
+        if (!((b >> (16 * t + i)) & 1u)) s[t][i] = -INFINITY;
   }
   // The reference m of a row moves only when a key exceeds it by more than 2^8,
   // so most chunks need no exchange between lanes and no rescaling; weights
   // stay below 2^8 and a row that has seen no key keeps m = -inf, l = 0, O = 0.
+  float top = -INFINITY;
 #pragma unroll
-  for (int r = 0; r < RG; ++r) {
-    float top = -INFINITY;
+  for (int t = 0; t < 2; ++t)
 #pragma unroll
-    for (int t = 0; t < 2; ++t)
+    for (int i = 0; i < 4; ++i) top = fmaxf(top, s[t][i]);
+  if (__any(top * c2 > st.m * c2 + 8.f)) {
+    top = fmaxf(top, __shfl_xor(top, 16));
+    top = fmaxf(top, __shfl_xor(top, 32));
+    const float m = top * c2 > st.m * c2 + 8.f ? top : st.m;
+    const float f = __builtin_amdgcn_exp2f((st.m - (m == -INFINITY ? 0.f : m)) * c2);
+    st.l *= f;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) top = fmaxf(top, s[r][t][i]);
-    if (__any(top * c2 > st.m[r] * c2 + 8.f)) {
-      top = fmaxf(top, __shfl_xor(top, 16));
-      top = fmaxf(top, __shfl_xor(top, 32));
-      const float m = top * c2 > st.m[r] * c2 + 8.f ? top : st.m[r];
-      const float f = __builtin_amdgcn_exp2f((st.m[r] - (m == -INFINITY ? 0.f : m)) * c2);
-      st.l[r] *= f;
-#pragma unroll
-      for (int t = 0; t < 8; ++t) st.o[r][t] *= f;
-      st.m[r] = m;
-    }
-    const float ref = -(st.m[r] == -INFINITY ? 0.f : st.m[r]) * c2;
-    bf16x8 w;
-#pragma unroll
-    for (int t = 0; t < 2; ++t)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) w[4 * t + i] = __bf16(__builtin_amdgcn_exp2f(fmaf(s[r][t][i], c2, ref)));
-    p[r] = __builtin_bit_cast(u32x4, w);
-    add_weights(p[r], st.l[r]);
+    for (int t = 0; t < 8; ++t) st.o[t] *= f;
+    st.m = m;
   }
+  const float ref = -(st.m == -INFINITY ? 0.f : st.m) * c2;
+  bf16x8 w;
+#pragma unroll
+  for (int t = 0; t < 2; ++t)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[4 * t + i] = __bf16(__builtin_amdgcn_exp2f(fmaf(s[t][i], c2, ref)));
+  p = __builtin_bit_cast(u32x4, w);
+  add_weights(p, st.l);
 }
 
 // O of a chunk.  V: dims 8 c + 2 j, 8 c + 2 j + 1 of eight keys, transposed.  A key
 // that is not there has zeros instead of what its memory holds: 0 * NaN is NaN.
-template <int RG, bool E8>
-__device__ __forceinline__ void chunk_values(const Chunk<RG, E8>& c, const uint32_t there, const u32x4 (&p)[RG], Rows<RG>& st) {
+template <bool E8>
+__device__ __forceinline__ void chunk_values(const Chunk<E8>& c, const uint32_t there, const u32x4& p, Rows& st) {
   const int g = (threadIdx.x & 63) >> 4;
   const uint32_t here = there >> (4 * g);
   const bool whole = there == ~0u;
@@ -255,11 +245,8 @@ __device__ __forceinline__ void chunk_values(const Chunk<RG, E8>& c, const uint3
       lo[x] = __builtin_amdgcn_perm(w[2 * x + 1], w[2 * x], 0x05040100u);
       hi[x] = __builtin_amdgcn_perm(w[2 * x + 1], w[2 * x], 0x07060302u);
     }
-#pragma unroll
-    for (int r = 0; r < RG; ++r) {
-      st.o[r][2 * j] = mfma16(lo, p[r], st.o[r][2 * j]);
-      st.o[r][2 * j + 1] = mfma16(hi, p[r], st.o[r][2 * j + 1]);
-    }
+    st.o[2 * j] = mfma16(lo, p, st.o[2 * j]);
+    st.o[2 * j + 1] = mfma16(hi, p, st.o[2 * j + 1]);
   }
 }
 
@@ -277,17 +264,17 @@ __device__ __forceinline__ Parts parts_of(const PagedArgs& a, int blocks) {
   return Parts{o, o + int64_t(blocks) * 2 * ROWS * kHead};
 }
 
-template <int RG, bool E8, int W>
-__global__ __launch_bounds__(64 * W, RG == 1 ? 8 / W : 1) void paged_attention(PagedArgs a, int whole) {
+template <bool E8, int W>
+__global__ __launch_bounds__(64 * W, 8 / W) void paged_attention(PagedArgs a, int whole) {
   constexpr int kWaves = W, kStep = kChunk * W;
-  __shared__ __attribute__((aligned(16))) float red[kWaves * RG * 8 * 64 * 4];
-  __shared__ float ml[kWaves][16 * RG][2];
+  __shared__ __attribute__((aligned(16))) float red[kWaves * 8 * 64 * 4];
+  __shared__ float ml[kWaves][16][2];
   const int lane = threadIdx.x & 63, c16 = lane & 15, g = lane >> 4;
   const int wave = uniform(threadIdx.x >> 6);
-  const int rows = a.budget * a.group, ntile = (rows + 16 * RG - 1) / (16 * RG);
+  const int rows = a.budget * a.group, ntile = (rows + 15) / 16;
   const int per = a.heads_kv * ntile;   // items of a request
   const int blocks = gridDim.x, blk = xcd_order(blockIdx.x, blocks);
-  const Parts parts = parts_of<16 * RG>(a, blocks);
+  const Parts parts = parts_of<16>(a, blocks);
   const int words = 2 * ((a.budget + 63) / 64);
   const int page_size = 1 << a.c.page_log2;
 
@@ -300,25 +287,20 @@ __global__ __launch_bounds__(64 * W, RG == 1 ? 8 / W : 1) void paged_attention(P
     const int n = min(left, steps - step);
     const int kvh = item / ntile, rt = item - kvh * ntile;
 
-    u32x4 qf[RG][4];
-    Rows<RG> st;
-    const uint32_t* mrow[RG];
-    int node[RG];
+    u32x4 qf[4];
+    Rows st;
+    const int row = min(rt * 16 + c16, rows - 1);   // past the end: the last row, never stored
+    const int node = row / a.group;
+    const int64_t from = (int64_t(q) * a.budget + node) * a.q_stride + (kvh * a.group + row - node * a.group) * kHead;
+    // operand ks: dims 64 (ks / 2) + 16 g + 8 (ks % 2) .. + 7, for keys alike
 #pragma unroll
-    for (int r = 0; r < RG; ++r) {
-      const int row = min(rt * 16 * RG + r * 16 + c16, rows - 1);   // past the end: the last row, never stored
-      node[r] = row / a.group;
-      const int64_t at = (int64_t(q) * a.budget + node[r]) * a.q_stride + (kvh * a.group + row - node[r] * a.group) * kHead;
-      // operand ks: dims 64 (ks / 2) + 16 g + 8 (ks % 2) .. + 7, for keys alike
+    for (int ks = 0; ks < 4; ++ks)
+      qf[ks] = *reinterpret_cast<const u32x4*>(a.q + from + 64 * (ks >> 1) + 16 * g + 8 * (ks & 1));
+    const uint32_t* mrow = a.mask ? reinterpret_cast<const uint32_t*>(a.mask) + (int64_t(q) * a.budget + node) * words : nullptr;
+    st.m = -INFINITY;
+    st.l = 0.f;
 #pragma unroll
-      for (int ks = 0; ks < 4; ++ks)
-        qf[r][ks] = *reinterpret_cast<const u32x4*>(a.q + at + 64 * (ks >> 1) + 16 * g + 8 * (ks & 1));
-      mrow[r] = a.mask ? reinterpret_cast<const uint32_t*>(a.mask) + (int64_t(q) * a.budget + node[r]) * words : nullptr;
-      st.m[r] = -INFINITY;
-      st.l[r] = 0.f;
-#pragma unroll
-      for (int t = 0; t < 8; ++t) st.o[r][t] = f32x4{0.f, 0.f, 0.f, 0.f};
-    }
+    for (int t = 0; t < 8; ++t) st.o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
 
     // The context: chunks of keys kb .. kb + 31, a step apart.  The next chunk's keys
     // are fetched once this one's scores are formed, its values once this one's
@@ -327,10 +309,9 @@ __global__ __launch_bounds__(64 * W, RG == 1 ? 8 / W : 1) void paged_attention(P
     const int kb0 = step * kStep + wave * kChunk;
     const int chunks = kb0 < ex.ctx ? min(min(step + n, nctx) - step, (ex.ctx - kb0 + kStep - 1) / kStep) : 0;
     if (chunks > 0) {
-      Chunk<RG, E8> ch;
-      f32x4 sc[RG][2];
-      u32x4 p[RG];
-      uint32_t vis[RG];
+      Chunk<E8> ch;
+      f32x4 sc[2];
+      u32x4 p;
       int p0, p1;   // pages of the halves of the chunk to fetch next
       auto look_up = [&](int kb) __attribute__((always_inline)) {
         p0 = table[kb >> a.c.page_log2];
@@ -383,12 +364,10 @@ __global__ __launch_bounds__(64 * W, RG == 1 ? 8 / W : 1) void paged_attention(P
         const int kb = kb0 + (i + 1) * kStep;
         const bool more = i + 1 < chunks;
         if (more) look_up(kb);
-        chunk_scores<RG, E8>(ch, qf, sc);
+        chunk_scores<E8>(ch, qf, sc);
         if (more) fetch_keys(kb);
-#pragma unroll
-        for (int r = 0; r < RG; ++r) vis[r] = there;
-        chunk_weights<RG>(sc, there != ~0u, vis, a.scale_log2, st, p);
-        chunk_values<RG, E8>(ch, there, p, st);
+        chunk_weights(sc, there != ~0u, there, a.scale_log2, st, p);
+        chunk_values<E8>(ch, there, p, st);
         if (more) fetch_values();
       }
     }
@@ -401,7 +380,7 @@ __global__ __launch_bounds__(64 * W, RG == 1 ? 8 / W : 1) void paged_attention(P
       auto at = [&](int key) {
         return (int64_t(q) * a.budget + min(kb + key, ex.nodes - 1)) * a.kv_stride + kvh * kHead;
       };
-      Chunk<RG, false> ch;
+      Chunk<false> ch;
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
         const uint16_t* kp = a.k_tree + at(16 * t + c16) + 16 * g;
@@ -412,74 +391,61 @@ __global__ __launch_bounds__(64 * W, RG == 1 ? 8 / W : 1) void paged_attention(P
 #pragma unroll
       for (int e = 0; e < 8; ++e)
         ch.v16[e] = *reinterpret_cast<const u32x4*>(a.v_tree + at(16 * (e >> 2) + 4 * g + (e & 3)) + 8 * c16);
-      uint32_t vis[RG];
-#pragma unroll
-      for (int r = 0; r < RG; ++r) {
-        if (mrow[r]) vis[r] = mrow[r][kb >> 5] & there;
-        else vis[r] = node[r] < kb ? 0u : (node[r] - kb >= 31 ? ~0u : (2u << (node[r] - kb)) - 1u) & there;
-      }
-      f32x4 sc[RG][2];
-      u32x4 p[RG];
-      chunk_scores<RG, false>(ch, qf, sc);
-      chunk_weights<RG>(sc, true, vis, a.scale_log2, st, p);
-      chunk_values<RG, false>(ch, there, p, st);
+      const uint32_t sees = mrow ? mrow[kb >> 5] : node < kb ? 0u : node - kb >= 31 ? ~0u : (2u << (node - kb)) - 1u;
+      f32x4 sc[2];
+      u32x4 p;
+      chunk_scores<false>(ch, qf, sc);
+      chunk_weights(sc, true, sees & there, a.scale_log2, st, p);
+      chunk_values<false>(ch, there, p, st);
     }
 
-    // join the four waves: their rows scaled to the block's maximum, added in wave order
-#pragma unroll
-    for (int r = 0; r < RG; ++r) {
-      float l = st.l[r];
-      l += __shfl_xor(l, 16);
-      l += __shfl_xor(l, 32);
-      if (g == 0) {
-        ml[wave][r * 16 + c16][0] = st.m[r];
-        ml[wave][r * 16 + c16][1] = l;
-      }
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-          *reinterpret_cast<f32x4*>(&red[(((wave * RG + r) * 8 + 2 * i + h) * 64 + lane) * 4]) =
-              f32x4{st.o[r][4 * h][i], st.o[r][4 * h + 1][i], st.o[r][4 * h + 2][i], st.o[r][4 * h + 3][i]};
+    // join the waves: their rows scaled to the block's maximum, added in wave order
+    float l = st.l;
+    l += __shfl_xor(l, 16);
+    l += __shfl_xor(l, 32);
+    if (g == 0) {
+      ml[wave][c16][0] = st.m;
+      ml[wave][c16][1] = l;
     }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        *reinterpret_cast<f32x4*>(&red[((wave * 8 + 2 * i + h) * 64 + lane) * 4]) =
+            f32x4{st.o[4 * h][i], st.o[4 * h + 1][i], st.o[4 * h + 2][i], st.o[4 * h + 3][i]};
     __syncthreads();
     const bool direct = n == steps;
     const int slot = 2 * blk + (step > 0 ? 0 : 1);
-    const int i4 = wave & 3;   // this wave: dims 32 g + 8 i4 .. + 7 of row groups wave / 4, + W / 4, ..
+    if (wave < 4) {   // a wave: dims 32 g + 8 wave .. + 7
+      float M = ml[0][c16][0];
 #pragma unroll
-    for (int r = 0; r < RG; ++r) {
-      if (r % (W / 4) != wave / 4) continue;
-      const int lr = r * 16 + c16, row = rt * 16 * RG + lr;
-      float M = ml[0][lr][0];
-#pragma unroll
-      for (int w = 1; w < kWaves; ++w) M = fmaxf(M, ml[w][lr][0]);
+      for (int w = 1; w < kWaves; ++w) M = fmaxf(M, ml[w][c16][0]);
       float L = 0.f;
       f32x4 v[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
       for (int w = 0; w < kWaves; ++w) {
-        const float mw = ml[w][lr][0];
+        const float mw = ml[w][c16][0];
         const float f = mw == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((mw - M) * a.scale_log2);
-        L += f * ml[w][lr][1];
+        L += f * ml[w][c16][1];
 #pragma unroll
         for (int h = 0; h < 2; ++h)
-          v[h] += f * *reinterpret_cast<const f32x4*>(&red[(((w * RG + r) * 8 + 2 * i4 + h) * 64 + lane) * 4]);
+          v[h] += f * *reinterpret_cast<const f32x4*>(&red[((w * 8 + 2 * wave + h) * 64 + lane) * 4]);
       }
-      if (row < rows) {
+      if (rt * 16 + c16 < rows) {
         if (direct) {
           const float inv = L > 0.f ? 1.f / L : 0.f;   // a row that sees nothing is zero
           bf16x8 o;
 #pragma unroll
           for (int i = 0; i < 8; ++i) o[i] = __bf16(v[i >> 2][i & 3] * inv);
-          const int nd = row / a.group;
-          const int64_t head = (int64_t(q) * a.budget + nd) * a.heads_q + kvh * a.group + row - nd * a.group;
-          *reinterpret_cast<bf16x8*>(a.out + head * kHead + 32 * g + 8 * i4) = o;
+          const int64_t head = (int64_t(q) * a.budget + node) * a.heads_q + kvh * a.group + row - node * a.group;
+          *reinterpret_cast<bf16x8*>(a.out + head * kHead + 32 * g + 8 * wave) = o;
         } else {
-          float* po = parts.o + (int64_t(slot) * 16 * RG + lr) * kHead + 32 * g + 8 * i4;
+          float* po = parts.o + (int64_t(slot) * 16 + c16) * kHead + 32 * g + 8 * wave;
           *reinterpret_cast<f32x4*>(po) = v[0];
           *reinterpret_cast<f32x4*>(po + 4) = v[1];
-          if (i4 == 0 && g == 0) {
-            parts.ml[(int64_t(slot) * 16 * RG + lr) * 2] = M;
-            parts.ml[(int64_t(slot) * 16 * RG + lr) * 2 + 1] = L;
+          if (wave == 0 && g == 0) {
+            parts.ml[(int64_t(slot) * 16 + c16) * 2] = M;
+            parts.ml[(int64_t(slot) * 16 + c16) * 2 + 1] = L;
           }
         }
       }
@@ -993,10 +959,10 @@ hipError_t launch_paged_attention(const PagedArgs& a, hipStream_t s) {
   const Plan p = plan_of(a.batch, a.budget, a.max_ctx, a.heads_q, a.heads_kv, a.eight);
   switch (p.kernel) {
     case kFew:
-      return a.eight ? launch<16, 128>(paged_attention<1, true, 4>, a, p, s) : launch<16, 128>(paged_attention<1, false, 4>, a, p, s);
+      return a.eight ? launch<16, 128>(paged_attention<true, 4>, a, p, s) : launch<16, 128>(paged_attention<false, 4>, a, p, s);
     case kFewWhole:
-      return a.eight ? launch<16, 256, 512>(paged_attention<1, true, 8>, a, p, s)
-                     : launch<16, 256, 512>(paged_attention<1, false, 8>, a, p, s);
+      return a.eight ? launch<16, 256, 512>(paged_attention<true, 8>, a, p, s)
+                     : launch<16, 256, 512>(paged_attention<false, 8>, a, p, s);
     case kTiles64:
       return a.eight ? launch<64, kTile>(paged_tiles<1, true, 4>, a, p, s) : launch<64, kTile>(paged_tiles<1, false, 4>, a, p, s);
     case kTiles128:

@@ -200,6 +200,23 @@ def test_many_large_trees(kind, n, hq, chain):
 
 
 @pytest.mark.parametrize("kind", [E8, BF])
+@pytest.mark.parametrize("n,hq,hkv,chain", [(1, 8, 2, True), (4, 8, 2, False), (16, 2, 2, True), (5, 16, 4, False),
+                                            (40, 4, 2, False), (33, 8, 2, True)])
+def test_keys_shared_out_over_blocks(kind, n, hq, hkv, chain):
+    """Contexts long enough that blocks cut items anywhere, over requests of all lengths."""
+    lens, nn = [3000, 0, 1, 2049, 700, 2999], [n, 0, n, 1, n, n]
+    holes = [(0, 0, -1), (0, 187, 1 << 20), (3, 60, -5), (3, 61, -1), (5, 187, -1)] + [(4, i, -1) for i in range(44)]
+    Case(6, n, 3000, hq, hkv, 16, kind, lens=lens, num_nodes=nn, chain=chain, strided=True, holes=holes, seed=12).check(heads=[0, hq - 1])
+
+
+@pytest.mark.parametrize("kind", [E8, BF])
+@pytest.mark.parametrize("b,n,ctx,hq,hkv,lens", [(3, 500, 2048, 32, 8, [2048, 0, 777]), (1, 512, 4000, 16, 8, [3999])])
+def test_few_large_trees_over_long_contexts(kind, b, n, ctx, hq, hkv, lens):
+    """Tiles of 128 query rows whose keys are shared out over blocks."""
+    Case(b, n, ctx, hq, hkv, 64, kind, lens=lens, num_nodes=[n, n - 370, 1][:b], holes=[(0, 7, -1)], seed=13).check(heads=[0, hq - 1])
+
+
+@pytest.mark.parametrize("kind", [E8, BF])
 @pytest.mark.parametrize("b,n,ctx", [(1, 1, 40000), (2, 16, 20011), (1, 64, 9000)])
 def test_long_contexts(kind, b, n, ctx):
     Case(b, n, ctx, 8, 2, 64, kind, seed=7).check(heads=[0, 7])
