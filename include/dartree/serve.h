@@ -99,9 +99,8 @@ dartree_status dartree_tree_attention_paged_workspace_size(const dartree_attn_pa
  * max_ctx; values are taken into 0 .. max_ctx) and to the nodes j < num_nodes[q]
  * (NULL: budget) whose bit is set in mask row i; mask NULL: j <= i, a chain
  * (budget 1: a single token).  Positions without a page and nodes at and past
- * num_nodes[q] are not seen, and what their memory holds does not matter; the
- * values of the nodes below it must be finite also for rows that do not see them
- * (their weight there is 0, and 0 times a NaN is a NaN).
+ * num_nodes[q] are not seen; what the memory of a key holds that a row does not
+ * see does not matter to that row, NaN and infinities included.
  * Every row i < budget is computed; one that sees nothing is 0.
  * a: as in dartree_tree_attention, with max_ctx <= max_pages * page, batch,
  * heads_kv and head_dim as in p; max_ctx is not limited otherwise.

@@ -47,6 +47,21 @@ __device__ __forceinline__ void add_weights(u32x4 w, float& sum) {
   for (int i = 0; i < 4; ++i) sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, uint32_t(w[i])), ones, sum, false);
 }
 
+// A tree's values that are no numbers must not reach rows that do not see them
+// (their weight there is 0, and 0 times a NaN is a NaN): they are multiplied as
+// zeros and added to the rows that do see them after the tree's last step.
+// odd_bits: bits 15 and 31 of the result are set where a half of w is an infinity
+// or a NaN.
+constexpr uint32_t kOdd = 0x80008000u;
+__device__ __forceinline__ uint32_t odd_bits(uint32_t w) { return (w & 0x7F807F80u) + 0x00800080u; }
+__device__ __forceinline__ uint32_t without_odd(uint32_t w) {
+  const uint32_t b = odd_bits(w);
+  return w & ~((b & 0x8000u ? 0xFFFFu : 0u) | (b & 0x80000000u ? 0xFFFF0000u : 0u));
+}
+__device__ __forceinline__ float odd_part(uint16_t v) {
+  return (v & 0x7F80u) == 0x7F80u ? __uint_as_float(uint32_t(v) << 16) : 0.f;
+}
+
 template <bool HI>
 __device__ __forceinline__ uint32_t expand2(uint32_t w, float scale) {
   return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, HI));
@@ -372,6 +387,10 @@ __global__ __launch_bounds__(64 * W, 8 / W) void paged_attention(PagedArgs a, in
       }
     }
     // the tree's own keys
+    auto sees = [&](int kb) {   // of kb .. kb + 31
+      return mrow ? mrow[kb >> 5] : node < kb ? 0u : node - kb >= 31 ? ~0u : (2u << (node - kb)) - 1u;
+    };
+    bool odd = false;   // the same for the wave
     for (int s = max(step, nctx); s < step + n; ++s) {
       const int kb = (s - nctx) * kStep + wave * kChunk;
       if (kb >= ex.nodes) break;
@@ -391,13 +410,39 @@ __global__ __launch_bounds__(64 * W, 8 / W) void paged_attention(PagedArgs a, in
 #pragma unroll
       for (int e = 0; e < 8; ++e)
         ch.v16[e] = *reinterpret_cast<const u32x4*>(a.v_tree + at(16 * (e >> 2) + 4 * g + (e & 3)) + 8 * c16);
-      const uint32_t sees = mrow ? mrow[kb >> 5] : node < kb ? 0u : node - kb >= 31 ? ~0u : (2u << (node - kb)) - 1u;
+      const uint32_t seen = sees(kb);
+      uint32_t bits = 0;
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) bits |= odd_bits(ch.v16[e][j]);
+      if (__any(bits & kOdd)) {
+        odd = true;
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) ch.v16[e][j] = without_odd(ch.v16[e][j]);
+      }
       f32x4 sc[2];
       u32x4 p;
       chunk_scores<false>(ch, qf, sc);
-      chunk_weights(sc, true, sees & there, a.scale_log2, st, p);
+      chunk_weights(sc, true, seen & there, a.scale_log2, st, p);
       chunk_values<false>(ch, there, p, st);
     }
+    if (odd)
+      for (int s = max(step, nctx); s < step + n; ++s) {
+        const int kb = (s - nctx) * kStep + wave * kChunk;
+        if (kb >= ex.nodes) break;
+        const uint32_t seen = sees(kb);
+        for (int key = 0; key < min(kChunk, ex.nodes - kb); ++key) {
+          if (!((seen >> key) & 1u)) continue;
+          const uint16_t* vp = a.v_tree + (int64_t(q) * a.budget + kb + key) * a.kv_stride + kvh * kHead + 32 * g;
+#pragma unroll
+          for (int t = 0; t < 8; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) st.o[t][i] += odd_part(vp[8 * i + t]);
+        }
+      }
 
     // join the waves: their rows scaled to the block's maximum, added in wave order
     float l = st.l;
@@ -499,6 +544,7 @@ struct Index {
 template <int RG, bool E8, int W>
 __global__ __launch_bounds__(64 * W, 8 / W) void paged_tiles(PagedArgs a, int whole) {
   __shared__ __attribute__((aligned(16))) char smem[4 * kTileBytes];   // [buffer][K, V]
+  __shared__ int odd;   // the last of the block's items (counted from 1) whose tree holds values that are no numbers
   LDS_AS char* const lds = (LDS_AS char*)smem;
   constexpr int kRows = 16 * W * RG;
   const int lane = threadIdx.x & 63, r16 = lane & 15, g = lane >> 4;
@@ -512,8 +558,10 @@ __global__ __launch_bounds__(64 * W, 8 / W) void paged_tiles(PagedArgs a, int wh
   Place at;
   if (!place_of<kTile>(a, whole, per, blk, blocks, &at)) return;
   int q = uniform(at.q), item = uniform(at.item), step = uniform(at.step), left = uniform(at.left);
+  if (threadIdx.x == 0) odd = 0;
+  __syncthreads();
 
-  while (left > 0) {
+  for (int turn = 1; left > 0; ++turn) {
     const Extent<kTile> ex = extent_at<kTile>(a, q);
     const int steps = ex.steps(), nctx = ex.ctx_steps();
     const int n = min(left, steps - step), last = step + n;
@@ -772,9 +820,14 @@ __global__ __launch_bounds__(64 * W, 8 / W) void paged_tiles(PagedArgs a, int wh
 #pragma unroll
         for (int i = 0; i < kShares; ++i) {
           const int key = 4 * W * i + key0;
+          if (!((in_flight >> key) & 1)) vx[i] = zero;
+          if ((odd_bits(vx[i][0]) | odd_bits(vx[i][1]) | odd_bits(vx[i][2]) | odd_bits(vx[i][3])) & kOdd) {
+            odd = turn;
+#pragma unroll
+            for (int x = 0; x < 4; ++x) vx[i][x] = without_odd(vx[i][x]);
+          }
           *reinterpret_cast<LDS_AS u32x4*>(kt + key * kRowBytes + (c ^ k_place(key)) * 16) = kx[i];
-          *reinterpret_cast<LDS_AS u32x4*>(kt + kTileBytes + key * kRowBytes + (c ^ v_place(key)) * 16) =
-              (in_flight >> key) & 1 ? vx[i] : zero;
+          *reinterpret_cast<LDS_AS u32x4*>(kt + kTileBytes + key * kRowBytes + (c ^ v_place(key)) * 16) = vx[i];
         }
 #pragma unroll
         for (int r = 0; r < RG; ++r) seen[r] = next_seen[r];
@@ -786,6 +839,28 @@ __global__ __launch_bounds__(64 * W, 8 / W) void paged_tiles(PagedArgs a, int wh
         return there & (d < 0 ? 0ull : d >= 63 ? ~0ull : (2ull << d) - 1);
       };
       sweep(max(step, nctx), last, fetch, store, sees, true);
+      // a wave that is ahead may have raised it for its next item: then nothing is found here
+      if (odd >= turn) {
+        for (int s = max(step, nctx); s < last; ++s) {
+          const int kb = (s - nctx) * kTile, valid = min(kTile, ex.nodes - kb);
+          if (valid <= 0) break;
+          const uint64_t there = valid == kTile ? ~0ull : (1ull << valid) - 1;
+#pragma unroll
+          for (int r = 0; r < RG; ++r) {
+            const int d = node[r] - kb;
+            const uint64_t sees = there & (a.mask ? a.mask[(int64_t(q) * a.budget + node[r]) * words + (s - nctx)]
+                                                  : d < 0 ? 0ull : d >= 63 ? ~0ull : (2ull << d) - 1);
+            for (int key = 0; key < valid; ++key) {
+              if (!((sees >> key) & 1)) continue;
+              const uint16_t* vp = a.v_tree + (int64_t(q) * a.budget + kb + key) * a.kv_stride + kvh * kHead + 4 * ((tid & 63) >> 4);
+#pragma unroll
+              for (int t = 0; t < 8; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) o[r][t][i] += odd_part(vp[16 * t + i]);
+            }
+          }
+        }
+      }
     }
 
     const bool direct = n == steps;
@@ -867,14 +942,15 @@ __global__ __launch_bounds__(256) void paged_join(PagedArgs a, int blocks) {
       o[i] = *reinterpret_cast<const f32x4*>(parts.o + p * kHead + d);
     }
     float top = M;
-    bool use[B];
+    bool use[B], any = false;   // a part without a seen key has a sum of 0 (of NaN where its only keys are)
 #pragma unroll
     for (int i = 0; i < B; ++i) {
       const int b = c0 + i;
-      use[i] = b <= b1 && !(sparse && total * b / blocks == total * (b + 1) / blocks) && ml[i][0] != -INFINITY;
+      use[i] = b <= b1 && !(sparse && total * b / blocks == total * (b + 1) / blocks) && ml[i][1] != 0.f;
+      any |= use[i];
       if (use[i]) top = fmaxf(top, ml[i][0]);
     }
-    if (top == -INFINITY) continue;
+    if (!any) continue;
     const float f = __builtin_amdgcn_exp2f((M - top) * a.scale_log2);
     L *= f;
     acc *= f;
@@ -939,11 +1015,17 @@ Plan plan_of(int batch, int budget, int max_ctx, int heads_q, int heads_kv, int 
   return p;
 }
 
-template <int ROWS, int STEP, int THREADS = 256, typename K>
+template <typename K>
+hipError_t launch_whole(K* kernel, int threads, const PagedArgs& a, const Plan& p, hipStream_t s) {
+  hipLaunchKernelGGL(kernel, dim3(p.blocks), dim3(threads), 0, s, a, 1);
+  return hipGetLastError();
+}
+template <int ROWS, int STEP, typename K>
 hipError_t launch(K* kernel, const PagedArgs& a, const Plan& p, hipStream_t s) {
-  hipLaunchKernelGGL(kernel, dim3(p.blocks), dim3(THREADS), 0, s, a, p.whole);
+  if (p.whole) return launch_whole(kernel, 256, a, p, s);
+  hipLaunchKernelGGL(kernel, dim3(p.blocks), dim3(256), 0, s, a, 0);
   const hipError_t e = hipGetLastError();
-  if (e != hipSuccess || p.whole) return e;
+  if (e != hipSuccess) return e;
   hipLaunchKernelGGL((paged_join<ROWS, STEP>), dim3(unsigned(p.items * (ROWS / 8))), dim3(256), 0, s, a, p.blocks);
   return hipGetLastError();
 }
@@ -961,15 +1043,13 @@ hipError_t launch_paged_attention(const PagedArgs& a, hipStream_t s) {
     case kFew:
       return a.eight ? launch<16, 128>(paged_attention<true, 4>, a, p, s) : launch<16, 128>(paged_attention<false, 4>, a, p, s);
     case kFewWhole:
-      return a.eight ? launch<16, 256, 512>(paged_attention<true, 8>, a, p, s)
-                     : launch<16, 256, 512>(paged_attention<false, 8>, a, p, s);
+      return a.eight ? launch_whole(paged_attention<true, 8>, 512, a, p, s) : launch_whole(paged_attention<false, 8>, 512, a, p, s);
     case kTiles64:
       return a.eight ? launch<64, kTile>(paged_tiles<1, true, 4>, a, p, s) : launch<64, kTile>(paged_tiles<1, false, 4>, a, p, s);
     case kTiles128:
       return a.eight ? launch<128, kTile>(paged_tiles<2, true, 4>, a, p, s) : launch<128, kTile>(paged_tiles<2, false, 4>, a, p, s);
     default:
-      return a.eight ? launch<256, kTile, 512>(paged_tiles<2, true, 8>, a, p, s)
-                     : launch<256, kTile, 512>(paged_tiles<2, false, 8>, a, p, s);
+      return a.eight ? launch_whole(paged_tiles<2, true, 8>, 512, a, p, s) : launch_whole(paged_tiles<2, false, 8>, 512, a, p, s);
   }
 }
 

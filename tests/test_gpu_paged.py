@@ -231,6 +231,34 @@ def test_equal_calls_give_equal_bits(b, n, ctx):
     assert torch.equal(first, c.run())
 
 
+@pytest.mark.parametrize("kind", [E8, BF])
+@pytest.mark.parametrize("b,n,ctx,hq,hkv,chain", [(2, 20, 100, 4, 2, False), (2, 12, 3000, 2, 2, True), (2, 70, 3000, 4, 2, False),
+                                                  (1, 512, 3000, 32, 8, False), (128, 64, 40, 32, 8, False)])
+def test_nodes_that_are_no_numbers(kind, b, n, ctx, hq, hkv, chain):
+    """Infinities and NaN in keys and values of tree nodes: rows that see such a node take them, the others do not."""
+    plain, odd = (Case(b, n, ctx, hq, hkv, 16, kind, chain=chain, seed=14) for _ in range(2))
+    nan, inf = float("nan"), float("inf")
+    bad = {n - 1: (inf, nan), n // 2: (0.0, -inf), n // 3: (0.0, inf), n // 5: (nan, 0.0)}   # node: key's element 3, value's element 77
+    for j, (k, v) in bad.items():
+        for c, kk, vv in ((odd, k, v), (plain, 0.0, 0.0)):
+            c.dk[:, j, :, 3] = kk
+            c.dv[:, j, :, 77] = vv
+    base, out = plain.run().double().cpu(), odd.run().double().cpu()
+    for q in {0, b // 2, b - 1}:
+        see = torch.from_numpy(odd.see[q])
+        lost = torch.zeros(n, dtype=torch.bool)                # rows that see a key that is no number
+        value = torch.zeros(n, dtype=torch.float64)            # what element 77 takes besides
+        for j, (k, v) in bad.items():
+            lost |= see[:, j] & (k != 0.0)
+            value += torch.where(see[:, j] & (v != 0.0), v, 0.0).double()
+        want = base[q].clone()
+        want[:, :, 77] += value[:, None]
+        kept = ~lost
+        assert kept.any() and torch.equal(out[q][kept].nan_to_num(), want[kept].nan_to_num())
+        assert torch.equal(out[q][kept].isnan(), want[kept].isnan()) and (value != 0).any()
+        assert not out[q][lost].isfinite().all(dim=-1).any()
+
+
 def test_follows_the_dense_layer():
     """The same attention as dartree_tree_attention on the context read back."""
     c = Case(2, 48, 300, 8, 2, 16, E8, lens=[300, 123], seed=9)
