@@ -151,7 +151,6 @@ __device__ __forceinline__ int wave_min_int(int x) {
   for (int off = 32; off > 0; off >>= 1) x = min(x, __shfl_xor(x, off));
   return x;
 }
-__device__ __forceinline__ int wave_max_int(int x) { return -wave_min_int(-x); }
 
 // A block's share of a segment in registers, and the segment's record from it
 // (table: kExp32 in LDS).
@@ -325,7 +324,11 @@ __device__ __forceinline__ int pick_in_segment(int seg, double target, F&& weigh
   if (lane == 63) wsum[wave] = incl;
   __syncthreads();
   double cum = incl - sum;
-  for (int x = 0; x < wave; ++x) cum += wsum[x];
+#pragma unroll
+  for (int x = 0; x < NT / 64; ++x) {   // all read at once
+    const double o = wsum[x];
+    cum += x < wave ? o : 0.0;
+  }
   int found = INT32_MAX, pos = -1;
 #pragma unroll
   for (int k = 0; k < kEach; ++k)
@@ -337,12 +340,10 @@ __device__ __forceinline__ int pick_in_segment(int seg, double target, F&& weigh
         if (found == INT32_MAX && cum > target) found = pos;
       }
     }
-  found = wave_min_int(found);
-  pos = wave_max_int(pos);
-  if (lane == 0) {
-    atomicMin(&got[0], found);   // whole numbers: the order does not matter
-    atomicMax(&got[1], pos);
-  }
+  // a wave's tokens rise with its lanes; whole numbers: the order of waves does not matter
+  const uint64_t hit = __ballot(found != INT32_MAX), some = __ballot(pos >= 0);
+  if (hit && lane == __builtin_ctzll(hit)) atomicMin(&got[0], found);
+  if (some && lane == 63 - __builtin_clzll(some)) atomicMax(&got[1], pos);
   __syncthreads();
   const int r = got[0];
   *last = got[1];
