@@ -85,24 +85,39 @@ __constant__ double kExp32[32] = {
 
 // The same for the many elements of a pass: exp((z - m) / T) = 2^(n / 32) 2^(f / 32),
 // |f| <= 1/2, from a table in LDS (32 entries take 64 banks: no conflicts) and a
-// series to degree 4 (the next term is below 2e-12).  NaN and -inf give 2^-1000,
-// nothing beside a sum that is at least 1.  z is at most m.
+// series to degree 4 (the next term is below 2e-12).  z is at most m.
 struct ExpTable {
   const double* table;   // LDS
-  double c32, mc32;      // 32 log2(e) / T, m times that
-  __device__ ExpTable(const double* t, double c, float m) : table(t), c32(32.0 * c), mc32(double(m) * (32.0 * c)) {}
-  __device__ void add(float z, double& sum) const {
+  double c32, m;         // 32 log2(e) / T
+  __device__ ExpTable(const double* t, double c, float mm) : table(t), c32(32.0 * c), m(mm) {}
+  // 2^(f / 32) from t = n + f
+  __device__ static double series(double t, int& n) {
     constexpr double kRound = 6755399441055744.0;   // 1.5 * 2^52: adding it leaves the nearest whole number in the low bits
-    const double t = fmax(fma(double(z), c32, -mc32), -32000.0);
     const double r = t + kRound, f = t - (r - kRound);
-    const int n = int(uint32_t(__builtin_bit_cast(uint64_t, r)));
+    n = int(uint32_t(__builtin_bit_cast(uint64_t, r)));
     double p = 9.172562701824643e-09;
     p = fma(p, f, 1.6938509724371819e-06);
     p = fma(p, f, 0.00023459619820224677);
     p = fma(p, f, 0.02166084939249829);
-    p = fma(p, f, 1.0);
+    return fma(p, f, 1.0);
+  }
+  __device__ double scaled(float z) const { return (double(z) - m) * c32; }   // the difference is exact
+  // The same with one operation less, m c32 rounded first: good to 2^-34 where that
+  // is below 2^20.  Takes NaN, not +inf.
+  __device__ bool near() const { return m < 3.40282347e+38 && fabs(m * c32) < 1048576.0; }
+  __device__ double scaled_near(float z) const { return fma(double(z), c32, -(m * c32)); }
+  // Added to a sum that is at least 1: NaN and -inf give 2^-1000, nothing beside it.
+  __device__ void add(double t, double& sum) const {
+    int n;
+    const double p = series(fmax(t, -32000.0), n);
     const uint64_t e = __builtin_bit_cast(uint64_t, table[n & 31]) + (uint64_t(uint32_t(n & ~31) << 15) << 32);
     sum = fma(__builtin_bit_cast(double, e), p, sum);
+  }
+  // by itself: 2^-1200 is 0 in 64 bits
+  __device__ double of(float z) const {
+    int n;
+    const double p = series(fmax(scaled(z), -38400.0), n);
+    return __builtin_ldexp(table[n & 31] * p, n >> 5);
   }
 };
 
@@ -196,16 +211,16 @@ __device__ __forceinline__ void segment_record(const Segment<BF, NT>& in, const 
           if (x[l][i] >= m) arg = min(arg, first[l] + i);
     } else {
       const ExpTable e(table, c, m);
-      if (m < 3.40282347e+38f) {
+      if (e.near()) {
 #pragma unroll
         for (int l = 0; l < L; ++l)
 #pragma unroll
-          for (int i = 0; i < N; ++i) e.add(x[l][i], s);
+          for (int i = 0; i < N; ++i) e.add(e.scaled_near(x[l][i]), s);
       } else {   // +inf counts as the largest number
 #pragma unroll
         for (int l = 0; l < L; ++l)
 #pragma unroll
-          for (int i = 0; i < N; ++i) e.add(sane(x[l][i]), s);
+          for (int i = 0; i < N; ++i) e.add(e.scaled(sane(x[l][i])), s);
       }
     }
   }
@@ -450,11 +465,12 @@ __global__ __launch_bounds__(256) void row_records(const void* z, int64_t zrows,
 constexpr int kShares = 64;
 template <bool BF, int NT>
 __device__ int final_token(const VerifyArgs& a, int64_t row, const Record* rec, int nseg, const Law& law, const int32_t* gone,
-                           const double* share, int ngone, float u, double* segw) {
+                           const double* share, int ngone, float u, double* segw, const double* table) {
   constexpr int N = RowView<BF>::N;
   const RowView<BF> z(a.target, row, a.row_stride, a.vocab);
   if (law.empty()) return -1;
   if (law.c == 0.0) return law.arg;   // all of the mass on one token: it remains, or nothing does and p decides
+  const ExpTable e(table, law.c, float(law.m));
   for (int pass = 0; pass < 2; ++pass) {   // second: nothing was left of p
     const int n = pass == 0 ? ngone : 0;
     bool again = false;
@@ -478,7 +494,7 @@ __device__ int final_token(const VerifyArgs& a, int64_t row, const Record* rec, 
       int first;
       z.load(chunk, x, first);
 #pragma unroll
-      for (int i = 0; i < N; ++i) w[i] = x[i] == -INFINITY ? 0.0 : law.weight(x[i], first + i);
+      for (int i = 0; i < N; ++i) w[i] = x[i] == -INFINITY ? 0.0 : e.of(x[i]);
       for (int k = 0; k < n; ++k) {
         const int d = gone[k] - first;
 #pragma unroll
@@ -511,12 +527,13 @@ __global__ __launch_bounds__(kWalkNodes) void tree_walk(VerifyArgs a, int nseg, 
   __shared__ float rm[kWalkNodes + 1];
   __shared__ int32_t rarg[kWalkNodes + 1];
   __shared__ double rs[kWalkNodes + 1];
-  __shared__ double segw[kMaxSeg];
+  __shared__ double segw[kMaxSeg], table[32];
   __shared__ int at_s, tested_s;
   const int q = blockIdx.x, B = a.budget;
   const int n = min(max(a.num_nodes[q], 0), B);
   const int lane = threadIdx.x & 63;
   const Record* qrec = rec + int64_t(q) * (B + 1) * nseg;
+  if (threadIdx.x < 32) table[threadIdx.x] = kExp32[threadIdx.x];
   // the drafted tokens' logits, then the rows' laws, then the tokens' shares
   const int j = threadIdx.x;
   float zj = -INFINITY;
@@ -593,7 +610,7 @@ __global__ __launch_bounds__(kWalkNodes) void tree_walk(VerifyArgs a, int nseg, 
   const int at = at_s;
   const Law law(Record{rm[at + 1], rarg[at + 1], rs[at + 1]}, c);
   const int t = final_token<BF, kWalkNodes>(a, int64_t(q) * (B + 1) + at + 1, qrec + int64_t(at + 1) * nseg, nseg, law, tok, share, tested_s,
-                                a.uniforms[int64_t(q) * (B + 1)], segw);
+                                a.uniforms[int64_t(q) * (B + 1)], segw, table);
   if (threadIdx.x == 0) a.bonus[q] = t;
 }
 
@@ -699,7 +716,7 @@ __device__ __forceinline__ void wave_record(const RowView<BF>& z, int seg, const
 #pragma unroll
       for (int i = 0; i < N; ++i) {
         if (c == 0.0) arg = x[i] == m ? min(arg, first + i) : arg;
-        else e.add(x[i], s);
+        else e.add(e.scaled(x[i]), s);
       }
     }
   if (c == 0.0) arg = wave_min_int(arg);
@@ -823,7 +840,7 @@ __global__ __launch_bounds__(kPathThreads) void path_walk(VerifyArgs a, int nseg
   for (int j = count + threadIdx.x; j < a.max_len; j += kPathThreads) a.accepted[int64_t(q) * a.max_len + j] = -1;
   __syncthreads();
   const int t = final_token<BF, kPathThreads>(a, int64_t(q) * (B + 1) + at + 1, qrec + int64_t(slot) * nseg, nseg, law, gone, share,
-                                              ngone, a.uniforms[int64_t(q) * (B + 1)], segw);
+                                              ngone, a.uniforms[int64_t(q) * (B + 1)], segw, table);
   if (threadIdx.x == 0) {
     a.num_accepted[q] = count;
     a.bonus[q] = t;
@@ -892,6 +909,7 @@ struct Residual {
   static constexpr int N = RowView<BF>::N;
   RowView<BF> z, y;
   Law p, q;
+  ExpTable ep, eq;
   double pn, qn;   // 1 / their wholes
   bool reject;
   __device__ int operator()(int chunk, double (&w)[N]) const {
@@ -899,7 +917,7 @@ struct Residual {
     int first;
     z.load(chunk, x, first);
 #pragma unroll
-    for (int i = 0; i < N; ++i) w[i] = x[i] == -INFINITY ? 0.0 : p.weight(x[i], first + i);
+    for (int i = 0; i < N; ++i) w[i] = x[i] == -INFINITY ? 0.0 : ep.of(x[i]);
     if (reject) {
       float v[N];
       if (y.shift == z.shift) {
@@ -911,20 +929,20 @@ struct Residual {
       }
 #pragma unroll
       for (int i = 0; i < N; ++i)
-        w[i] = fmax(w[i] * pn - (q.empty() || v[i] == -INFINITY ? 0.0 : q.weight(v[i], first + i) * qn), 0.0);
+        w[i] = fmax(w[i] * pn - (q.empty() || v[i] == -INFINITY ? 0.0 : eq.of(v[i]) * qn), 0.0);
     }
     return first;
   }
 };
 template <bool BF>
-__device__ __forceinline__ Residual<BF> residual_of(const VerifyArgs& a, double c, const ChainRows& rows, int n) {
+__device__ __forceinline__ Residual<BF> residual_of(const VerifyArgs& a, double c, const ChainRows& rows, int n, const double* table) {
   const int q = blockIdx.y, D = a.budget, k = rows.count;
   const bool reject = k < n && c != 0.0;
   const int d = reject ? n + 1 + k : 0;
   return Residual<BF>{RowView<BF>(a.target, int64_t(q) * (D + 1) + k, a.row_stride, a.vocab),
                       RowView<BF>(a.draft, reject ? int64_t(q) * D + k : 0, a.row_stride, a.vocab),
                       Law(Record{rows.m[k], rows.arg[k], rows.s[k]}, c), Law(Record{rows.m[d], rows.arg[d], rows.s[d]}, c),
-                      1.0 / rows.s[k], 1.0 / rows.s[d], reject};
+                      ExpTable(table, c, rows.m[k]), ExpTable(table, c, rows.m[d]), 1.0 / rows.s[k], 1.0 / rows.s[d], reject};
 }
 
 // The final token: block (segment, request).  After a rejection every block
@@ -935,11 +953,12 @@ __global__ __launch_bounds__(kPick) void chain_final(VerifyArgs a, int nseg, dou
                                                      uint64_t* segw, int32_t* arrived) {
   constexpr int N = RowView<BF>::N;
   __shared__ ChainRows rows;
-  __shared__ double sw[kMaxSeg];
+  __shared__ double sw[kMaxSeg], table[32];
   __shared__ int last_s;
   const int q = blockIdx.y, D = a.budget;
+  if (threadIdx.x < 32) table[threadIdx.x] = kExp32[threadIdx.x];
   const int n = chain_walk<BF>(a, nseg, c, trec, drec, rows);
-  Residual<BF> f = residual_of<BF>(a, c, rows, n);
+  Residual<BF> f = residual_of<BF>(a, c, rows, n, table);
   int t = -1;
   if (f.reject && !f.p.empty()) {
     const double sum = segment_weight<kPick, N>(blockIdx.x, f);

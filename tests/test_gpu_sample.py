@@ -204,6 +204,25 @@ def test_tree_edges_along_paths():
     check_tree(tokens, parents, np.full(12, -5), z, 1.0, u, 8)
 
 
+@pytest.mark.parametrize("budget", [8, 1025])
+@pytest.mark.parametrize("offset,temperature", [(1e5, 1e-2), (-3e7, 4.0), (2e30, 1e30), (-3e38, 1e37), (1e30, 1.0), (-1e12, 1e-3)])
+def test_large_logits(budget, offset, temperature):
+    """Logits far from 0 and wide apart: what counts is their exact difference over the temperature."""
+    rng = np.random.default_rng(15)
+    vocab, b = 5000, 6
+    tokens, parents = random_trees(rng, b, budget, vocab, spine=0.5, kids=4)
+    step = np.spacing(np.float32(abs(offset)))             # whole steps of the type, a few temperatures wide
+    spread = max(1.0, temperature / step)
+    with np.errstate(over="ignore"):                       # some become -inf
+        z = (offset + np.round(rng.normal(size=(b, budget + 1, vocab)) * 2.0 * spread) * float(step)).astype(np.float32)
+    for q in range(b):
+        for j in range(min(budget, 200)):
+            z[q, parents[q, j] + 1, tokens[q, j]] = z[q, parents[q, j] + 1].max()
+    check_tree(tokens, parents, np.full(b, budget), z, temperature, rng.random((b, budget + 1)).astype(np.float32), 8)
+    d, v, n = z[:, :5], z[:, 1:5], np.full(b, 4)
+    check_chain(tokens[:, :4], n, d, v, temperature, rng.random((b, 5)).astype(np.float32))
+
+
 def test_tree_little_mass_left():
     """Children that hold all but 1e-7 .. 1e-14 of the mass, tested with the largest random number."""
     rng = np.random.default_rng(12)
