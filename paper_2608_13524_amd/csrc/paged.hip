@@ -901,14 +901,46 @@ __global__ __launch_bounds__(64 * W, 8 / W) void paged_tiles(PagedArgs a, int wh
   }
 }
 
-// Join the partial results of the items that were cut: block (item, eight of its
-// rows), 32 lanes per row.  Eight blocks' results are loaded together and folded
-// in block order.
-template <int ROWS, int STEP>
+// A row's partial result while parts are folded into it in order.  A part without
+// a seen key has a sum of 0 (of NaN where its only keys are).
+struct Folded {
+  float m, l;
+  f32x4 o;
+};
+template <int N>
+__device__ __forceinline__ void fold(Folded& r, const bool (&use)[N], const float (&m)[N], const float (&l)[N], const f32x4 (&o)[N],
+                                     float c2) {
+  float top = r.m;
+  bool any = false;
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+    if (use[i] && l[i] != 0.f) {
+      any = true;
+      top = fmaxf(top, m[i]);
+    }
+  if (!any) return;
+  const float f = __builtin_amdgcn_exp2f((r.m - top) * c2);
+  r.l = r.l == 0.f ? 0.f : r.l * f;
+  r.o *= r.l == 0.f ? 0.f : f;
+  r.m = top;
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+    if (use[i] && l[i] != 0.f) {
+      const float w = __builtin_amdgcn_exp2f((m[i] - top) * c2);
+      r.l += w * l[i];
+      r.o += o[i] * w;
+    }
+}
+
+// Join the partial results of the items that were cut: block (item, 8 / G of its
+// rows), 32 lanes for each G-th of a row's parts.  B parts are loaded together
+// and folded in block order, then the G results.
+template <int ROWS, int STEP, int G>
 __global__ __launch_bounds__(256) void paged_join(PagedArgs a, int blocks) {
+  constexpr int R = 8 / G, B = G == 1 ? 8 : 4;
   const int rows = a.budget * a.group, ntile = (rows + ROWS - 1) / ROWS, per = a.heads_kv * ntile;
-  const int part = blockIdx.x % (ROWS / 8);
-  const int it = blockIdx.x / (ROWS / 8);
+  const int part = blockIdx.x % (ROWS / R);
+  const int it = blockIdx.x / (ROWS / R);
   const int q = it / per, item = it - q * per;
   const int lane = threadIdx.x & 63;
   int64_t total = 0, before = 0;
@@ -923,51 +955,62 @@ __global__ __launch_bounds__(256) void paged_join(PagedArgs a, int blocks) {
   const int b0 = int(((first + 1) * blocks - 1) / total), b1 = int(((first + steps) * blocks - 1) / total);
   if (b0 == b1) return;
   const int kvh = item / ntile, rt = item - kvh * ntile;
-  const int lr = part * 8 + (threadIdx.x >> 5), row = rt * ROWS + lr, d = 4 * (threadIdx.x & 31);
-  if (row >= rows) return;
+  const int group = threadIdx.x >> 5;
+  const int lr = part * R + group % R, row = rt * ROWS + lr, d = 4 * (threadIdx.x & 31);
+  if (row >= rows) return;   // G > 1: the whole block
   const Parts parts = parts_of<ROWS>(a, blocks);
-  float M = -INFINITY, L = 0.f;
-  f32x4 acc{0.f, 0.f, 0.f, 0.f};
-  constexpr int B = 8;
+  const int each = (b1 - b0 + G) / G, c1 = G == 1 ? b1 : min(b0 + (group + 1) * each - 1, b1);
+  Folded r{-INFINITY, 0.f, f32x4{0.f, 0.f, 0.f, 0.f}};
   typedef float f32x2 __attribute__((ext_vector_type(2)));
   const bool sparse = total < blocks;   // fewer steps than blocks: some have none
-  for (int c0 = b0; c0 <= b1; c0 += B) {
-    f32x2 ml[B];
+  for (int c0 = G == 1 ? b0 : b0 + group * each; c0 <= c1; c0 += B) {
+    float m[B], l[B];
     f32x4 o[B];
+    bool use[B];
 #pragma unroll
     for (int i = 0; i < B; ++i) {
-      const int b = min(c0 + i, b1);
+      const int b = min(c0 + i, c1);
       const int64_t p = int64_t(2 * b + (b == b0 ? 1 : 0)) * ROWS + lr;
-      ml[i] = *reinterpret_cast<const f32x2*>(parts.ml + 2 * p);
+      const f32x2 ml = *reinterpret_cast<const f32x2*>(parts.ml + 2 * p);
       o[i] = *reinterpret_cast<const f32x4*>(parts.o + p * kHead + d);
+      m[i] = ml[0];
+      l[i] = ml[1];
     }
-    float top = M;
-    bool use[B], any = false;   // a part without a seen key has a sum of 0 (of NaN where its only keys are)
 #pragma unroll
     for (int i = 0; i < B; ++i) {
       const int b = c0 + i;
-      use[i] = b <= b1 && !(sparse && total * b / blocks == total * (b + 1) / blocks) && ml[i][1] != 0.f;
-      any |= use[i];
-      if (use[i]) top = fmaxf(top, ml[i][0]);
+      use[i] = b <= c1 && !(sparse && total * b / blocks == total * (b + 1) / blocks);
     }
-    if (!any) continue;
-    const float f = __builtin_amdgcn_exp2f((M - top) * a.scale_log2);
-    L *= f;
-    acc *= f;
-    M = top;
-#pragma unroll
-    for (int i = 0; i < B; ++i)
-      if (use[i]) {
-        const float w = __builtin_amdgcn_exp2f((ml[i][0] - top) * a.scale_log2);
-        L += w * ml[i][1];
-        acc += o[i] * w;
-      }
+    fold(r, use, m, l, o, a.scale_log2);
   }
-  const float inv = L > 0.f ? 1.f / L : 0.f;
+  if constexpr (G > 1) {
+    __shared__ f32x4 go[G][32];
+    __shared__ float gm[G], gl[G];
+    go[group][threadIdx.x & 31] = r.o;
+    if ((threadIdx.x & 31) == 0) {
+      gm[group] = r.m;
+      gl[group] = r.l;
+    }
+    __syncthreads();
+    if (group > 0) return;
+    float m[G], l[G];
+    f32x4 o[G];
+    bool use[G];
+#pragma unroll
+    for (int i = 0; i < G; ++i) {
+      m[i] = gm[i];
+      l[i] = gl[i];
+      o[i] = go[i][threadIdx.x];
+      use[i] = true;
+    }
+    r = Folded{-INFINITY, 0.f, f32x4{0.f, 0.f, 0.f, 0.f}};
+    fold(r, use, m, l, o, a.scale_log2);
+  }
+  const float inv = r.l > 0.f ? 1.f / r.l : r.l;   // a row that sees nothing is zero
   const int node = row / a.group;
   uint16_t* out = a.out + ((int64_t(q) * a.budget + node) * a.heads_q + kvh * a.group + row - node * a.group) * kHead + d;
   typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
-  *reinterpret_cast<bf16x4*>(out) = bf16x4{__bf16(acc[0] * inv), __bf16(acc[1] * inv), __bf16(acc[2] * inv), __bf16(acc[3] * inv)};
+  *reinterpret_cast<bf16x4*>(out) = bf16x4{__bf16(r.o[0] * inv), __bf16(r.o[1] * inv), __bf16(r.o[2] * inv), __bf16(r.o[3] * inv)};
 }
 
 // Which kernel, its tile's query rows and the blocks of a launch: as many as the
@@ -1026,7 +1069,15 @@ hipError_t launch(K* kernel, const PagedArgs& a, const Plan& p, hipStream_t s) {
   hipLaunchKernelGGL(kernel, dim3(p.blocks), dim3(256), 0, s, a, 0);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((paged_join<ROWS, STEP>), dim3(unsigned(p.items * (ROWS / 8))), dim3(256), 0, s, a, p.blocks);
+  // Many parts an item are shared out over eight groups of lanes, which takes eight
+  // times the blocks (us, with one group / eight, 32 / 8 heads: 16 rows, 64 parts,
+  // one token over 8192 positions 19.3 / 14.1; 16 parts, 4 tokens over 16384 36.9 /
+  // 35.7; 64 rows, 32 parts, 2 x 16 nodes over 65536 116.5 / 116.1; 16 parts, 64
+  // nodes over 8192 32.0 / 32.9).
+  if (p.blocks > std::max(8, ROWS / 4) * p.items)
+    hipLaunchKernelGGL((paged_join<ROWS, STEP, 8>), dim3(unsigned(p.items * ROWS)), dim3(256), 0, s, a, p.blocks);
+  else
+    hipLaunchKernelGGL((paged_join<ROWS, STEP, 1>), dim3(unsigned(p.items * (ROWS / 8))), dim3(256), 0, s, a, p.blocks);
   return hipGetLastError();
 }
 
