@@ -619,7 +619,7 @@ __global__ __launch_bounds__(kWalkNodes) void tree_walk(VerifyArgs a, int nseg, 
 // along the best children from the current node are read in one launch, and a
 // walk goes on until it leaves them.  kRounds of that, the first with the few rows
 // that most trees end in, and the last walk reads the rows it still lacks by
-// itself (a block per request, 30 us a row): a sampled path leaves the best
+// itself (a block per request, tens of microseconds a row): a sampled path leaves the best
 // children seldom and then ends soon.  16 trees of 512 nodes of depth 16, vocab
 // 151936 fp32: 2 rounds of 17 rows 83.9 us, of 8 and 17 88.2, a third round 78.4,
 // a fourth 82.9.  One node a launch, its last block walking on, took 194.
@@ -692,36 +692,47 @@ __global__ __launch_bounds__(256) void path_records(VerifyArgs a, int nseg, int 
   segment_record<BF, 256>(s, table, c, rec + (int64_t(q) * nrows + i) * nseg + seg);
 }
 
-// A segment's record by one wave.
+// A segment's record by one wave, in one pass: every lane keeps the maximum of its
+// elements and the sum beside it.
 template <bool BF>
 __device__ __forceinline__ void wave_record(const RowView<BF>& z, int seg, const double* table, double c, Record* out) {
-  constexpr int N = RowView<BF>::N, L = kSeg / N / 64;
+  constexpr int N = RowView<BF>::N, L = kSeg / N / 64, H = 16 / N;
   float m = -INFINITY;
-  for (int l = 0; l < L; ++l) {
-    float x[N];
-    int first;
-    z.load(seg * (kSeg / N) + l * 64 + (threadIdx.x & 63), x, first);
-#pragma unroll
-    for (int i = 0; i < N; ++i) m = fmaxf(m, x[i]);
-  }
-  m = wave_max(m);
   int arg = INT32_MAX;
   double s = 0.0;
-  const ExpTable e(table, c, m);
-  if (m != -INFINITY)
-    for (int l = 0; l < L; ++l) {
-      float x[N];
-      int first;
-      z.load(seg * (kSeg / N) + l * 64 + (threadIdx.x & 63), x, first);
+#pragma unroll 1
+  for (int l = 0; l < L; l += H) {
+    float x[H][N], top = m;
+    int first[H];
+#pragma unroll
+    for (int h = 0; h < H; ++h) z.load(seg * (kSeg / N) + (l + h) * 64 + (threadIdx.x & 63), x[h], first[h]);
+#pragma unroll
+    for (int h = 0; h < H; ++h)
+#pragma unroll
+      for (int i = 0; i < N; ++i) top = fmaxf(top, x[h][i]);
+    if (top == -INFINITY) continue;
+    if (top > m) {
+      s = m == -INFINITY ? 0.0 : s * exp64((double(m) - double(top)) * c);
+      arg = INT32_MAX;
+      m = top;
+    }
+    const ExpTable e(table, c, m);
+#pragma unroll
+    for (int h = 0; h < H; ++h)
 #pragma unroll
       for (int i = 0; i < N; ++i) {
-        if (c == 0.0) arg = x[i] == m ? min(arg, first + i) : arg;
-        else e.add(e.scaled(x[i]), s);
+        if (c == 0.0) arg = x[h][i] == m ? min(arg, first[h] + i) : arg;
+        else e.add(e.scaled(x[h][i]), s);
       }
-    }
+  }
+  const float whole = wave_max(m);
+  if (m != whole) {
+    s = m == -INFINITY ? 0.0 : s * exp64((double(m) - double(whole)) * c);
+    arg = INT32_MAX;
+  }
   if (c == 0.0) arg = wave_min_int(arg);
   else s = wave_sum64(s);
-  if ((threadIdx.x & 63) == 0) *out = Record{m, c == 0.0 ? arg : 0, s};
+  if ((threadIdx.x & 63) == 0) *out = Record{whole, c == 0.0 ? arg : 0, s};
 }
 
 // The first child of `at` whose token is taken, -1: none (one wave).  FILL: the
