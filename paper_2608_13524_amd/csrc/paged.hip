@@ -1030,10 +1030,10 @@ Plan plan_of(int batch, int budget, int max_ctx, int heads_q, int heads_kv, int 
   // Few 16-row items with few keys: a block of eight waves takes each, with no
   // partial results and no second launch.  A compute unit draws about 47 GB/s,
   // 1.4 us per 256 keys of e4m3.  Whole / shared (us, 32 / 8 heads, e4m3 unless
-  // said): 1 request x 64 nodes, 512 positions 10 / 18, 2048 20 / 22 (bf16 25 /
+  // said): 1 request x 64 nodes, 512 positions 10 / 18, 2048 18 / 22 (bf16 25 /
   // 22), 4096 32 / 26; 4 x 64 x 1024 26 / 27, 8 x 64 x 1024 48 / 36; 4 x 16 x
-  // 2048 20 / 23; single tokens: 1 x 512 9 / 10, 1 x 2048 18 / 12, 4 x 2048 19 /
-  // 15, 16 x 2048 19 / 21.
+  // 2048 20 / 23; single tokens: 1 x 512 8 / 10, 1 x 2048 18 / 10, 4 x 2048 19 /
+  // 14, 16 x 2048 18 / 21.
   const int64_t turns = ((int64_t(max_ctx) + budget + 255) / 256) * (eight ? 1 : 2), few = tiles_of(16);
   if (few <= 512 && (turns <= 3 || (turns <= 4 && rows > 16) || (turns <= 9 && few <= 256 && (rows > 16 || few >= 128)))) {
     p.kernel = kFewWhole;

@@ -190,6 +190,27 @@ def test_steps_on_another_stream():
         assert loops[1].same_as(loops[0]) and loops[2].same_as(loops[0])
 
 
+def test_two_loops_at_once():
+    """Steps of two loops in flight on two streams, each with workspaces of its own."""
+    rng = np.random.default_rng(8)
+    pair, alone = [Loop(Shared(k), 10 + k) for k in (E8, BF)], [Loop(Shared(k), 10 + k) for k in (E8, BF)]
+    streams = [torch.cuda.Stream() for _ in pair]
+    us = [[uniforms(rng) for _ in pair] for _ in range(4)]
+    say("two loops at once")
+    torch.cuda.synchronize()
+    for u in us:
+        for loop, stream, x in zip(pair, streams, u):
+            with torch.cuda.stream(stream):
+                loop.u.copy_(x)
+                loop.step()
+    torch.cuda.synchronize()
+    for u in us:
+        for loop, x in zip(alone, u):
+            loop.u.copy_(x)
+            loop.step()
+    assert pair[0].same_as(alone[0]) and pair[1].same_as(alone[1])
+
+
 def test_a_stream_of_another_device_is_refused():
     class Elsewhere:
         device_index, cuda_stream = 1, 0
