@@ -1035,14 +1035,20 @@ Plan plan_of(int batch, int budget, int max_ctx, int heads_q, int heads_kv, int 
   // 2048 20 / 23; single tokens: 1 x 512 8 / 10, 1 x 2048 18 / 10, 4 x 2048 19 /
   // 14, 16 x 2048 18 / 21.
   const int64_t turns = ((int64_t(max_ctx) + budget + 255) / 256) * (eight ? 1 : 2), few = tiles_of(16);
-  if (few <= 512 && (turns <= 3 || (turns <= 4 && rows > 16) || (turns <= 9 && few <= 256 && (rows > 16 || few >= 128)))) {
+  // At most 64 items of 16 rows over middle contexts: shared out as for few rows
+  // (us, 1 request, 32 / 8 heads, whole or tiles of 64 rows / this way): 8 nodes,
+  // 1280 positions 12.8 / 10.7, 2048 16.9 / 12.1, 16000 22.1 / 18.9, 32768 in bf16
+  // 41 / 47; 16 x 4096 20.5 / 16.3, 16000 25.2 / 25.3; 32 x 1280 13.2 / 15.2, 2048 17.5 / 15.9, 4096
+  // 21.4 / 19.5, 8192 26.0 / 25.8.
+  const bool middle = rows > 16 && few <= 64 && turns > (few <= 32 ? 4 : 8) && turns <= (few <= 32 ? 64 : 32);
+  if (!middle && few <= 512 && (turns <= 3 || (turns <= 4 && rows > 16) || (turns <= 9 && few <= 256 && (rows > 16 || few >= 128)))) {
     p.kernel = kFewWhole;
     p.rows = 16;
     p.items = p.blocks = int(few);
     p.whole = 1;
     return p;
   }
-  const int step = rows <= 16 ? 128 : kTile;
+  const int step = rows <= 16 || middle ? 128 : kTile;
   const int64_t steps = (int64_t(max_ctx) + step - 1) / step + (budget + step - 1) / step;
   // 128 rows a tile (two groups a wave) double a tile's products per byte from LDS,
   // and a cut item's partial results; worth it where blocks take eight steps and
@@ -1050,7 +1056,7 @@ Plan plan_of(int batch, int budget, int max_ctx, int heads_q, int heads_kv, int 
   // whole items fill the chip and few of their rows are idle (16 x 512 nodes x 2048
   // positions, 32 / 8 heads: 371 us, with 128 rows 397, with 64 531).
   const bool wide = tiles_of(256) >= 1024 && 10 * 256 * tiles_of(256) <= 11 * 128 * tiles_of(128);
-  p.kernel = rows <= 16 ? kFew : rows <= 64 || tiles_of(128) * steps < 8 * kResident ? kTiles64 : wide ? kTiles256 : kTiles128;
+  p.kernel = rows <= 16 || middle ? kFew : rows <= 64 || tiles_of(128) * steps < 8 * kResident ? kTiles64 : wide ? kTiles256 : kTiles128;
   p.rows = p.kernel == kFew ? 16 : p.kernel == kTiles64 ? 64 : p.kernel == kTiles128 ? 128 : 256;
   p.items = tiles_of(p.rows);
   p.whole = p.kernel == kTiles256 || p.items >= 4 * kResident;

@@ -210,6 +210,15 @@ def test_keys_shared_out_over_blocks(kind, n, hq, hkv, chain):
 
 
 @pytest.mark.parametrize("kind", [E8, BF])
+@pytest.mark.parametrize("b,n,ctx,hq,hkv,chain", [(1, 8, 2048, 16, 4, False), (3, 33, 1500, 4, 2, False), (2, 100, 2500, 2, 1, True),
+                                                  (1, 16, 4000, 32, 8, True)])
+def test_few_items_over_middle_contexts(kind, b, n, ctx, hq, hkv, chain):
+    """More than 16 query rows a head whose 16-row items are cut."""
+    Case(b, n, ctx, hq, hkv, 32, kind, lens=[ctx, 1, ctx - 77][:b], num_nodes=[n, n, n - 5][:b], chain=chain, strided=True,
+         holes=[(0, 3, -1)], seed=16).check(heads=[0, hq - 1])
+
+
+@pytest.mark.parametrize("kind", [E8, BF])
 @pytest.mark.parametrize("b,n,ctx,hq,hkv,lens", [(3, 500, 2048, 32, 8, [2048, 0, 777]), (1, 512, 4000, 16, 8, [3999])])
 def test_few_large_trees_over_long_contexts(kind, b, n, ctx, hq, hkv, lens):
     """Tiles of 128 query rows whose keys are shared out over blocks."""
