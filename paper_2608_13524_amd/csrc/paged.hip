@@ -8,7 +8,7 @@
 // item cut by a block's end leaves partial results, which a second launch joins
 // in block order.
 //
-// Up to 16 query rows of a key/value head, or few keys (paged_attention): a step
+// Up to 16 query rows of a key/value head, or few items (paged_attention): a step
 // is a chunk of 32 keys for each of the block's four or eight waves, and a wave
 // works from registers alone.  S^T = K Q^T leaves lane (c = lane % 16, g = lane / 16) with
 // query c's weights of keys 4 g .. 4 g + 3 of both 16-key tiles, the B operand of
