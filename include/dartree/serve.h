@@ -82,8 +82,9 @@ dartree_status dartree_cache_write(const dartree_cache_params* p, const dartree_
 /* Read positions back as dense bf16: k, v [b][rows][heads_kv][128], row i of
  * request q is position start[q] + i for i < counts[q] (NULL as above), the
  * layout dartree_tree_attention takes its context in.  Exact: e4m3 times a
- * power of two fits bf16.  Positions without a page are zeros; rows at and
- * past counts[q] are left as they were. */
+ * power of two fits bf16, but for +-2^128: the numbers from 248 * 2^120 (3.30e38)
+ * on are held as that, and are read as bf16's largest, 255 * 2^120.  Positions
+ * without a page are zeros; rows at and past counts[q] are left as they were. */
 dartree_status dartree_cache_read(const dartree_cache_params* p, const dartree_cache* cache, int32_t rows, void* k,
                                   void* v, const int32_t* counts, const int32_t* start, hipStream_t stream);
 
@@ -107,10 +108,11 @@ dartree_status dartree_tree_attention_paged_workspace_size(const dartree_attn_pa
  * q: bf16, node i of request r at (r * budget + i) * q_stride elements,
  * heads_q * 128 each; k_tree, v_tree: likewise with kv_stride and heads_kv;
  * strides are multiples of 8.  out: bf16 [b][budget][heads_q][128].
- * Products of bf16 values (e4m3 keys and values are exact in bf16) with fp32
- * accumulation, fp32 softmax; the weights are rounded to bf16 for the
- * weighted sum of values, the output to bf16.  The order of sums is fixed by
- * the arguments: equal calls give equal bits. */
+ * Products of bf16 values (e4m3 keys and values as dartree_cache_read gives
+ * them) with fp32 accumulation, fp32 softmax; the weights are rounded to bf16 for
+ * the weighted sum of values, the output to bf16.  Weights are at most 2^8 before
+ * they are divided by their sum: values below 2^89 cannot overflow it.  The order
+ * of sums is fixed by the arguments: equal calls give equal bits. */
 dartree_status dartree_tree_attention_paged(const dartree_attn_params* a, const dartree_cache_params* p,
                                             const dartree_cache* cache, const void* q, int64_t q_stride,
                                             const void* k_tree, const void* v_tree, int64_t kv_stride,

@@ -89,8 +89,8 @@ __global__ __launch_bounds__(256) void cache_write(CacheMoveArgs a) {
 }
 
 // Eight e4m3 elements times the power of two of exponent byte e, in bf16.
-__device__ __forceinline__ u32x4 expand(u32x2 x, uint8_t e) {
-  const float s = __uint_as_float(uint32_t(e) << 23);
+__device__ __forceinline__ u32x4 expand(u32x2 x, uint32_t e) {
+  const float s = __uint_as_float(e << 23);
   u32x4 out;
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
@@ -115,8 +115,18 @@ __global__ __launch_bounds__(256) void cache_read(CacheMoveArgs a) {
     const int64_t row = slot + (int64_t(head) << a.c.page_log2);
     const int64_t from = row * kHead + lane * 8;
     if (E8) {
-      k = expand(*reinterpret_cast<const u32x2*>(static_cast<const uint8_t*>(a.c.k) + from), a.c.k_exp[row]);
-      v = expand(*reinterpret_cast<const u32x2*>(static_cast<const uint8_t*>(a.c.v) + from), a.c.v_exp[row]);
+      const u32x2 xk = *reinterpret_cast<const u32x2*>(static_cast<const uint8_t*>(a.c.k) + from);
+      const u32x2 xv = *reinterpret_cast<const u32x2*>(static_cast<const uint8_t*>(a.c.v) + from);
+      const uint32_t ek = a.c.k_exp[row], ev = a.c.v_exp[row];
+      k = expand(xk, ek);
+      v = expand(xv, ev);
+      if (max(ek, ev) >= kTopByte) {   // once, behind all loads
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          k[i] = finite_pair(k[i]);
+          v[i] = finite_pair(v[i]);
+        }
+      }
     } else {
       k = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(a.c.k) + from);
       v = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(a.c.v) + from);

@@ -10,6 +10,17 @@ namespace dartree {
 constexpr int kHead = 128;   // elements of a head
 constexpr int kExpLow = -100;   // least exponent of an e4m3 row
 
+// Exponent bytes from here on can stand for 2^128, which no bf16 or fp32 number
+// is: the e4m3 numbers nearest to 248 .. 255 times 2^120, bf16's largest, are 256
+// times that.  Rows with such a byte are converted with the largest bf16 number in
+// the place of an infinity (a NaN stays one).
+constexpr uint32_t kTopByte = 127 + 120;
+__device__ __forceinline__ uint32_t finite_pair(uint32_t w) {   // two bf16
+  if ((w & 0x7FFFu) == 0x7F80u) w -= 1;
+  if ((w & 0x7FFF0000u) == 0x7F800000u) w -= 0x10000u;
+  return w;
+}
+
 // A cache as the kernels see it.
 struct CacheView {
   int batch, heads_kv, page_log2, num_pages, max_pages;
