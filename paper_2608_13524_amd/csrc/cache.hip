@@ -45,8 +45,10 @@ __device__ __forceinline__ u32x2 quantise(u32x4 x, int& e) {
     f[2 * i + 1] = high(x[i]);
     m = fmaxf(m, fmaxf(fabsf(f[2 * i]), fabsf(f[2 * i + 1])));
   }
-  e = row_exponent(row16_max(m));
-  const float s = __uint_as_float(uint32_t(127 - e) << 23);   // 2^-e
+  m = row16_max(m);
+  e = row_exponent(m);
+  // 2^-e; with an infinity in the row 0, which makes that a NaN and the other values 0
+  const float s = m == INFINITY ? 0.f : __uint_as_float(uint32_t(127 - e) << 23);
   u32x2 out;
 #pragma unroll
   for (int i = 0; i < 2; ++i) {

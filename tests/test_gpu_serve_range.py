@@ -91,3 +91,27 @@ def test_attention_over_largest_numbers(n, ctx, hq, hkv, b):
             want = S.attention(q[r, :, h].astype(np.float64), kk, vv, see, float(np.float32(0.125)))
             tol = (2.0 ** -8 + 2.0 ** -9) * np.abs(vv).max(axis=0) + 2.0 ** -8 * np.abs(want)
             assert (np.abs(got[r, :, h] - want) <= tol).all(), (r, h)
+
+
+def test_large_numbers_beside_an_infinity():
+    """An e4m3 row with an infinity holds a NaN in its place and zeros elsewhere, whatever the other numbers."""
+    dev = device()
+    p = D.CacheParams(1, 1, 128, 16, 1, 1, E8)
+    c = make_cache(p, np.zeros((1, 1), int))
+    x = np.zeros((4, 128), np.float32)
+    x[:, :6] = [1e38, -3.38e38, 2.0 ** 112, -2.0 ** 111, 2.0 ** 109, 1.0]
+    x[0, 9], x[1, 9], x[2, 9] = np.inf, -np.inf, np.inf
+    x[2, 10], x[3, 9] = np.nan, np.nan
+    put = torch.from_numpy(x).to(dev).bfloat16().view(1, 4, 1, 128)
+    say("cache_write of large numbers beside an infinity")
+    D.cache_write(p, c, put, put, 4)
+    out = [torch.ones(1, 4, 1, 128, dtype=torch.bfloat16, device=dev) for _ in range(2)]
+    D.cache_read(p, c, *out)
+    torch.cuda.synchronize()
+    want = np.zeros((4, 128))
+    want[:, 9] = want[2, 10] = np.nan
+    rest = S.bf16(x[3]).astype(np.float64)
+    rest[9] = 0.0
+    want[3, :9] = held(rest[None])[0, :9]              # a NaN alone changes nothing else
+    for o in out:
+        assert np.array_equal(o.double().cpu().numpy()[0, :, 0], want, equal_nan=True)
