@@ -68,8 +68,9 @@ dartree_status dartree_cache_validate(const dartree_cache_params* p);
  *
  * E4M3: a row of 128 is held as e4m3(x * 2^-e), nearest even, with the least
  * e >= -100 for which the row's largest magnitude is at most 448 * 2^e (e =
- * -100 for a row of zeros); exp = e + 127.  Only values below 2^-15 of the
- * row's largest fall into e4m3's subnormals.
+ * -100 for a row of zeros); exp = e + 127.  Above e = -100 only values below
+ * 2^-13.8 of the row's largest fall into e4m3's subnormals (a row's largest is
+ * held above 224, the least normal number is 2^-6).
  * A NaN stays one; an infinity becomes one, and the other values of its row 0.
  *
  * Within a call, no two (request, position) pairs may share a slot.  Slots
