@@ -126,7 +126,9 @@ dartree_status dartree_tree_attention_paged(const dartree_attn_params* a, const 
  * and all mass on the first largest logit at T = 0.  A NaN logit counts as
  * -inf, +inf as the largest finite number; a row without any mass (all -inf)
  * accepts nothing and its token is -1.  logits_type: DARTREE_FP32 or
- * DARTREE_BF16.  Probabilities, sums and comparisons are taken in 64 bits. */
+ * DARTREE_BF16.  Sums, quotients and comparisons are taken in 64 bits, the
+ * exponentials are good to 3e-12: a result can differ from the definition's only
+ * where it hangs on less than 3e-11 of a row's mass. */
 
 /* Bytes of device workspace for dartree_verify_tree / dartree_verify_chain
  * (host only). */

@@ -4,7 +4,7 @@
 // A row of logits is cut into segments of 4096 elements (counted from the 16
 // bytes its start lies in, so that every load is aligned).  A segment's record
 // is its maximum, the maximum's first index and the sum of exp((z - max) / T).
-// Exponentials and sums are taken in 64 bits: the final token is where the
+// Sums are taken in 64 bits and exponentials to 3e-12: the final token is where the
 // cumulated mass passes u of the whole, and with 32 bits (1e-7) one draw in
 // sixty of a flat 151936-token row would land on a neighbour.  The vector units
 // do 64-bit fused multiply-adds at the 32-bit rate, and ExpTable needs eleven of
