@@ -92,7 +92,10 @@ dartree_status dartree_cache_read(const dartree_cache_params* p, const dartree_c
 /* ---- attention over the cache ---------------------------------------------- */
 
 /* Bytes of device workspace for dartree_tree_attention_paged (host only):
- * partial results where keys are shared out over blocks. */
+ * partial results where keys are shared out over blocks, at most 65 MiB.  The size
+ * belongs to these parameters: fewer requests, nodes or positions can need more
+ * (0 where every block takes whole items).  A loop over several sizes keeps the
+ * largest of their answers. */
 dartree_status dartree_tree_attention_paged_workspace_size(const dartree_attn_params* a, const dartree_cache_params* p,
                                                            size_t* bytes);
 
@@ -131,7 +134,8 @@ dartree_status dartree_tree_attention_paged(const dartree_attn_params* a, const 
  * where it hangs on less than 3e-11 of a row's mass. */
 
 /* Bytes of device workspace for dartree_verify_tree / dartree_verify_chain
- * (host only). */
+ * (host only).  That of trees, too, belongs to these sizes: smaller ones can need
+ * more (all rows' records instead of those of some paths). */
 dartree_status dartree_verify_tree_workspace_size(int32_t batch, int32_t budget, int32_t max_len, int32_t vocab,
                                                   size_t* bytes);
 dartree_status dartree_verify_chain_workspace_size(int32_t batch, int32_t depth, int32_t vocab, size_t* bytes);

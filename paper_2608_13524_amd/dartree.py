@@ -718,6 +718,7 @@ def cache_read(p: CacheParams, cache: DeviceCache, k, v, counts=None, start=None
 
 
 def tree_attention_paged_workspace_size(a: AttnParams, p: CacheParams) -> int:
+    """Bytes for these parameters; smaller ones can need more, so a loop over several keeps the largest answer."""
     n = ctypes.c_size_t(0)
     _check(lib().dartree_tree_attention_paged_workspace_size(ctypes.byref(a), ctypes.byref(p), ctypes.byref(n)),
            "dartree_tree_attention_paged_workspace_size")
@@ -751,6 +752,7 @@ def tree_attention_paged(a: AttnParams, p: CacheParams, cache: DeviceCache, q, k
 
 
 def verify_tree_workspace_size(batch: int, budget: int, max_len: int, vocab: int) -> int:
+    """Bytes for these sizes; smaller ones can need more."""
     n = ctypes.c_size_t(0)
     _check(lib().dartree_verify_tree_workspace_size(batch, budget, max_len, vocab, ctypes.byref(n)),
            "dartree_verify_tree_workspace_size")

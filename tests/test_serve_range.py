@@ -1,6 +1,7 @@
 """Numbers that serve.h states of the cache's 8-bit rows and of the verification's arithmetic."""
 import numpy as np
 
+from paper_2608_13524_amd import dartree as D
 from tests import serve_ref as S
 
 
@@ -27,3 +28,15 @@ def test_accuracy_of_the_exponentials():
     off = np.abs(series / np.exp2(f / 32) - 1).max()
     assert 1e-12 < off < 1.3e-12
     assert off + 2.0 ** -34 * np.log(2.0) / 32 + 2.0 ** -38 * np.log(2.0) / 32 * 3 < 3e-12
+
+
+def test_a_workspace_belongs_to_its_sizes():
+    """Smaller calls can need more than larger ones; never more than 65 MiB for attention."""
+    def attention(b, n, ctx, heads=(32, 8)):
+        return D.tree_attention_paged_workspace_size(D.AttnParams(b, n, ctx, *heads, 128, 0.1),
+                                                     D.CacheParams(b, heads[1], 128, 64, 10, ctx // 64, D.CACHE_E4M3))
+    assert attention(16, 512, 2048) == 0 < attention(8, 512, 2048)
+    most = max(attention(b, n, ctx, heads) for b in (1, 3, 8, 64) for n in (1, 4, 16, 33, 100, 512, 4096)
+               for ctx in (64, 1024, 4096, 65536) for heads in ((32, 8), (8, 8), (8, 1)))
+    assert most == 65 << 20
+    assert D.verify_tree_workspace_size(4, 64, 16, 151936) < D.verify_tree_workspace_size(2, 64, 16, 151936)
