@@ -19,8 +19,6 @@ constexpr size_t kAlign = 256;
 
 size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
 
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
 size_t act_bytes(int precision) { return precision == DARTREE_BF16 ? 2 : 4; }
 
 // Level sizes n_d = min(W, n_{d-1} k), n_0 = 1, and derived extents.
@@ -151,7 +149,7 @@ dartree_status check_tree(const dartree_tree* t) {
 
 dartree_status check_ws(const dartree_params& p, const void* ws, size_t ws_bytes, Layout* out) {
   const Layout l = layout_of(p, shape_of(p));
-  if (!ws || (reinterpret_cast<uintptr_t>(ws) % kAlign) != 0 || ws_bytes < l.total) return DARTREE_ERR_WORKSPACE;
+  if (!workspace_fits(ws, ws_bytes, l.total)) return DARTREE_ERR_WORKSPACE;
   *out = l;
   return DARTREE_OK;
 }
@@ -164,8 +162,6 @@ template <typename T>
 const T* at(const void* base, size_t off) {
   return reinterpret_cast<const T*>(static_cast<const char*>(base) + off);
 }
-
-dartree_status hip_status(hipError_t e) { return e == hipSuccess ? DARTREE_OK : DARTREE_ERR_HIP; }
 
 // ---------------------------------------------------------------------------
 // Depth order (Algorithm 1's loop runs d = 1..L, each depth reading the level
@@ -509,7 +505,7 @@ HeapLayout heap_layout_of(const dartree_params& p) {
 
 dartree_status check_heap_ws(const dartree_params& p, const void* ws, size_t ws_bytes, HeapLayout* out) {
   const HeapLayout l = heap_layout_of(p);
-  if (!ws || (reinterpret_cast<uintptr_t>(ws) % kAlign) != 0 || ws_bytes < l.total) return DARTREE_ERR_WORKSPACE;
+  if (!workspace_fits(ws, ws_bytes, l.total)) return DARTREE_ERR_WORKSPACE;
   *out = l;
   return DARTREE_OK;
 }
@@ -786,8 +782,7 @@ dartree_status dartree_project(int32_t precision, int32_t rows, int32_t vocab, i
   if (!x || !U || !bias || !z || !aligned16(x) || !aligned16(U) || !aligned16(z)) return DARTREE_ERR_INVALID_ARG;
   if (precision == DARTREE_BF16 && hidden % 64 != 0) return DARTREE_ERR_UNSUPPORTED;
   const size_t need = proj_split_bytes(precision, EPI_LOGITS, rows, vocab, hidden);
-  if (need > 0 && (!ws || (reinterpret_cast<uintptr_t>(ws) % kAlign) != 0 || ws_bytes < need))
-    return DARTREE_ERR_WORKSPACE;
+  if (!workspace_fits(ws, ws_bytes, need)) return DARTREE_ERR_WORKSPACE;
   ProjArgs a{};
   a.precision = precision;
   a.epilogue = EPI_LOGITS;
@@ -949,8 +944,7 @@ dartree_status dartree_tree_attention(const dartree_attn_params* p, const void* 
       (v_ctx && !aligned16(v_ctx)) || !aligned16(out))
     return DARTREE_ERR_INVALID_ARG;
   const AttnLayout l = attn_layout_of(*p);
-  if (l.total > 0 && (!ws || (reinterpret_cast<uintptr_t>(ws) % kAlign) != 0 || ws_bytes < l.total))
-    return DARTREE_ERR_WORKSPACE;
+  if (!workspace_fits(ws, ws_bytes, l.total)) return DARTREE_ERR_WORKSPACE;
   AttnArgs a{};
   a.batch = p->batch;
   a.budget = p->budget;

@@ -137,8 +137,6 @@ __global__ __launch_bounds__(1024) void calib_grid_barrier(int nbar, uint32_t* c
   __syncthreads();
 }
 
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
 // Enough workgroups for several per CU on 256 CUs, within the sink.
 unsigned stream_grid(int64_t n16) {
   const int64_t want = (n16 + kThreads * kUnroll - 1) / (kThreads * kUnroll);

@@ -34,6 +34,13 @@ inline int device_cus() {
   return n;
 }
 
+// Checks and results of the C ABI (host).
+inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+inline bool workspace_fits(const void* ws, size_t bytes, size_t need) {
+  return need == 0 || (ws && (reinterpret_cast<uintptr_t>(ws) % 256) == 0 && bytes >= need);
+}
+inline dartree_status hip_status(hipError_t e) { return e == hipSuccess ? DARTREE_OK : DARTREE_ERR_HIP; }
+
 // bfloat16 <-> fp32 on raw 16-bit patterns (finite values; nearest-even).
 __device__ __forceinline__ float bf16_to_f32(uint16_t b) { return __uint_as_float(uint32_t(b) << 16); }
 __device__ __forceinline__ uint16_t f32_to_bf16(float f) {

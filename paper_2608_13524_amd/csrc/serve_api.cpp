@@ -8,16 +8,8 @@ using namespace dartree;
 
 namespace {
 
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 bool given(const void* p) { return p && aligned16(p); }
 bool optional(const void* p) { return !p || aligned16(p); }
-
-dartree_status hip_status(hipError_t e) { return e == hipSuccess ? DARTREE_OK : DARTREE_ERR_HIP; }
-
-dartree_status check_ws(const void* ws, size_t bytes, size_t need) {
-  if (need > 0 && (!ws || (reinterpret_cast<uintptr_t>(ws) % 256) != 0 || bytes < need)) return DARTREE_ERR_WORKSPACE;
-  return DARTREE_OK;
-}
 
 dartree_status check_cache(const dartree_cache_params* p) {
   if (!p) return DARTREE_ERR_INVALID_ARG;
@@ -162,9 +154,9 @@ dartree_status dartree_tree_attention_paged(const dartree_attn_params* a, const 
   if (!stride_ok(q_stride, int64_t(a->heads_q) * kHead) || !stride_ok(kv_stride, int64_t(a->heads_kv) * kHead))
     return DARTREE_ERR_INVALID_ARG;
   const int eight = p->type == DARTREE_CACHE_E4M3;
-  if ((s = check_ws(ws, ws_bytes,
-                    paged_attention_workspace(a->batch, a->budget, a->max_ctx, a->heads_q, a->heads_kv, eight))) != DARTREE_OK)
-    return s;
+  if (!workspace_fits(ws, ws_bytes,
+                      paged_attention_workspace(a->batch, a->budget, a->max_ctx, a->heads_q, a->heads_kv, eight)))
+    return DARTREE_ERR_WORKSPACE;
   PagedArgs g{};
   g.c = view_of(*p, *cache);
   g.eight = eight;
@@ -216,7 +208,7 @@ dartree_status dartree_verify_tree(int32_t batch, int32_t budget, int32_t max_le
       !given(accepted) || !given(num_accepted) || !given(bonus))
     return DARTREE_ERR_INVALID_ARG;
   if (row_stride < vocab || row_stride > (int64_t(1) << 40)) return DARTREE_ERR_INVALID_ARG;
-  if ((s = check_ws(ws, ws_bytes, verify_tree_workspace(batch, budget, max_len, vocab))) != DARTREE_OK) return s;
+  if (!workspace_fits(ws, ws_bytes, verify_tree_workspace(batch, budget, max_len, vocab))) return DARTREE_ERR_WORKSPACE;
   VerifyArgs a{};
   a.batch = batch;
   a.budget = budget;
@@ -248,7 +240,7 @@ dartree_status dartree_verify_chain(int32_t batch, int32_t depth, int32_t vocab,
       !given(bonus) || !(temperature > 0.f ? given(draft_logits) : optional(draft_logits)))
     return DARTREE_ERR_INVALID_ARG;
   if (row_stride < vocab || row_stride > (int64_t(1) << 40)) return DARTREE_ERR_INVALID_ARG;
-  if ((s = check_ws(ws, ws_bytes, verify_chain_workspace(batch, depth, vocab))) != DARTREE_OK) return s;
+  if (!workspace_fits(ws, ws_bytes, verify_chain_workspace(batch, depth, vocab))) return DARTREE_ERR_WORKSPACE;
   VerifyArgs a{};
   a.batch = batch;
   a.budget = depth;

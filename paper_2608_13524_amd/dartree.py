@@ -644,9 +644,6 @@ class DeviceCache:
     v_exp: object
     table: object
 
-    def c(self) -> CacheC:
-        return CacheC(_ptr(self.k), _ptr(self.v), _ptr(self.k_exp), _ptr(self.v_exp), _ptr(self.table))
-
     @staticmethod
     def alloc(p: CacheParams, device="cuda") -> "DeviceCache":
         """Pages of undefined contents; every table entry -1 (no page)."""
