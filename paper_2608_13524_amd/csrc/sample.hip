@@ -619,8 +619,8 @@ __global__ __launch_bounds__(kWalkNodes) void tree_walk(VerifyArgs a, int nseg, 
 // along the best children from the current node are read in one launch, and a
 // walk goes on until it leaves them.  kRounds of that, the first with the few rows
 // that most trees end in, and the last walk reads the rows it still lacks by
-// itself (a block per request, tens of microseconds a row): a sampled path leaves the best
-// children seldom and then ends soon.  16 trees of 512 nodes of depth 16, vocab
+// itself (a block per request, 45 us a row of 151936): a target that agrees with the
+// drafter leaves the best children seldom (by_path has both kinds).  16 trees of 512 nodes of depth 16, vocab
 // 151936 fp32: 2 rounds of 17 rows 83.9 us, of 8 and 17 88.2, a third round 78.4,
 // a fourth 82.9.  One node a launch, its last block walking on, took 194.
 constexpr int kFirstRows = 8;   // rows of the first round
@@ -1007,17 +1007,29 @@ __global__ __launch_bounds__(kPick) void chain_final(VerifyArgs a, int nseg, dou
 constexpr size_t kAlign = 256;
 size_t up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
 
-// Rows of a request's path in a round, and whether to go by paths: that is worth
-// its launches once it leaves 64 MB of logits unread (counted as fp32: the
-// workspace is sized without the type).  Every row / by paths, us, path_rows 17:
-//   batch 1, 64 nodes, vocab 151936, 29 MB unread    24.3 / 26.6
-//   batch 16, 64 nodes, vocab 32000, 98 MB           45.3 / 43.6
-//   batch 4, 64 nodes, vocab 151936, 117 MB          54.5 / 45.3
-//   batch 1, 512 nodes, vocab 151936, 301 MB         93.9 / 26.2
-//   batch 16, 512 nodes, vocab 151936, 4.8 GB        1200 / 78.4
+// Rows of a request's path in a round, and whether to go by paths.  The rows along
+// the best children are read together, but after kRounds departures from them a
+// block reads each further row by itself, 45 us at a vocabulary of 151936.  So the
+// gain depends on the target: every row / by paths (us, path_rows 17, fp32), where it
+// follows the best child 85 % of the time, and where every node has two children
+// that hold 95 % in equal parts (full trees):
+//   batch x nodes x vocab, unread            best child    equal children
+//   1 x 64 x 151936, 29 MB                    25 / 28         24 / 53
+//   16 x 64 x 32000, 98 MB                    43 / 44         43 / 93
+//   4 x 64 x 151936, 117 MB                   52 / 45         51 / 101
+//   6 x 64 x 151936, 175 MB                   75 / 44         65 / 129
+//   8 x 64 x 151936, 233 MB                   87 / 51         87 / 146
+//   1 x 512 x 151936, 301 MB                  94 / 26         95 / 155
+//   16 x 64 x 151936, 466 MB                 164 / 60        160 / 178
+//   4 x 512 x 151936, 1.2 GB                 294 / 52        293 / 263
+//   16 x 512 x 151936, 4.8 GB               1200 / 77       1200 / 344
+// Past the border, 150 MB, the one gains about the factor that the other loses (as fp32:
+// the workspace is sized without the type).  The worst walk, 16 accepted nodes that
+// are none of them their parent's best child, takes 630 to 700 us at this vocabulary and
+// 240 to 270 at 32000.
 int path_rows(int budget, int max_len) { return std::min({kPathRows, max_len + 1, budget + 1}); }
 bool by_path(int batch, int budget, int max_len, int vocab) {
-  return budget > kWalkNodes || 4.0 * vocab * batch * (budget + 1 - path_rows(budget, max_len)) > 64e6;
+  return budget > kWalkNodes || 4.0 * vocab * batch * (budget + 1 - path_rows(budget, max_len)) > 150e6;
 }
 struct PathLayout {
   size_t walk, zd, child, rec, total;

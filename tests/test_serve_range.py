@@ -39,4 +39,4 @@ def test_a_workspace_belongs_to_its_sizes():
     most = max(attention(b, n, ctx, heads) for b in (1, 3, 8, 64) for n in (1, 4, 16, 33, 100, 512, 4096)
                for ctx in (64, 1024, 4096, 65536) for heads in ((32, 8), (8, 8), (8, 1)))
     assert most == 65 << 20
-    assert D.verify_tree_workspace_size(4, 64, 16, 151936) < D.verify_tree_workspace_size(2, 64, 16, 151936)
+    assert D.verify_tree_workspace_size(8, 64, 16, 151936) < D.verify_tree_workspace_size(4, 64, 16, 151936)
