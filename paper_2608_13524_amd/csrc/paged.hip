@@ -1100,10 +1100,15 @@ Plan plan_of(int batch, int budget, int max_ctx, int heads_q, int heads_kv, int 
   const int64_t steps = (int64_t(max_ctx) + step - 1) / step + (budget + step - 1) / step;
   // 128 rows a tile (two groups a wave) double a tile's products per byte from LDS,
   // and a cut item's partial results; worth it where blocks take eight steps and
-  // more.  256 rows (eight waves) halve the work of storing tiles; worth it where
-  // whole items fill the chip and few of their rows are idle (16 x 512 nodes x 2048
-  // positions, 32 / 8 heads: 371 us, with 128 rows 397, with 64 531).
-  const bool wide = tiles_of(256) >= 1024 && 10 * 256 * tiles_of(256) <= 11 * 128 * tiles_of(128);
+  // more.  256 rows (eight waves, an item a block) halve the work of storing tiles;
+  // worth it from three quarters of an item a compute unit on, where few of their
+  // rows are idle.  128 rows / 256 rows (us, 512 nodes over 2048 positions, 32 / 8
+  // heads, e4m3, 64 items of 256 rows a request; whole and ragged contexts):
+  // 2 requests 89 / 101, 3 127 / 107 and 116 / 101, 4 137 / 115 and 140 / 100, 5 191 /
+  // 197, 8 255 / 215 and 244 / 191, 12 367 / 313 and 365 / 290, 16 435 / 397 and 405 /
+  // 375, 17 468 / 480, 32 ragged 741 / 707; 4 over 500 positions 69 / 53, over 16000
+  // 632 / 575; bf16 alike.
+  const bool wide = tiles_of(256) >= 192 && 10 * 256 * tiles_of(256) <= 11 * 128 * tiles_of(128);
   p.kernel = rows <= 16 || middle ? kFew : rows <= 64 || tiles_of(128) * steps < 8 * kResident ? kTiles64 : wide ? kTiles256 : kTiles128;
   p.rows = p.kernel == kFew ? 16 : p.kernel == kTiles64 ? 64 : p.kernel == kTiles128 ? 128 : 256;
   p.items = tiles_of(p.rows);
