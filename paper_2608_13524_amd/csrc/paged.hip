@@ -17,8 +17,9 @@
 // t of the product is then dims 8 c + t, and a lane ends with dims 32 g .. 32 g + 31
 // of its query.  A tile lies in one page, so every load has a scalar base and an
 // offset that is the lane's own.  Keys in e4m3 become bf16 on the way with their
-// power of two applied by the conversion (exact).  Every key and value byte is
-// read once and never passes through LDS.
+// power of two applied by the conversion (exact).  A head's keys and values are read
+// once for 16 query rows (again for the next 16, from a cache where it holds them)
+// and never pass through LDS.
 //
 // More rows (paged_tiles): below.
 #include <algorithm>
@@ -38,8 +39,12 @@ __device__ __forceinline__ f32x4 mfma16(u32x4 a, u32x4 b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
 
-// sum += eight bf16 weights, in 32 bits: the rounded ones, as they multiply the
-// values, so that a common rounding cancels; two a lane and instruction.
+// sum += eight bf16 weights, in 32 bits, two a lane and instruction.  Weights are
+// rounded to bf16 because the matrix instructions multiply pairs of one 16-bit type
+// (in two parts they would take twice the products and their operands); the rounded
+// ones are summed, as they multiply the values, so that a common rounding cancels.
+// At most 2^-8 of a weight, so 2^-8 of the largest value in a result, whose own
+// rounding to bf16 is up to 2^-8 of it; the dense layer rounds its weights alike.
 __device__ __forceinline__ void add_weights(u32x4 w, float& sum) {
   typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
   const bf16x2 ones = __builtin_bit_cast(bf16x2, 0x3F803F80u);
@@ -1078,10 +1083,13 @@ Plan plan_of(int batch, int budget, int max_ctx, int heads_q, int heads_kv, int 
   // Few 16-row items with few keys: a block of eight waves takes each, with no
   // partial results and no second launch.  A compute unit draws about 47 GB/s,
   // 1.4 us per 256 keys of e4m3.  Whole / shared (us, 32 / 8 heads, e4m3 unless
-  // said): 1 request x 64 nodes, 512 positions 10 / 18, 2048 18 / 22 (bf16 25 /
-  // 22), 4096 32 / 26; 4 x 64 x 1024 26 / 27, 8 x 64 x 1024 48 / 36; 4 x 16 x
-  // 2048 20 / 23; single tokens: 1 x 512 8 / 10, 1 x 2048 18 / 10, 4 x 2048 19 /
-  // 14, 16 x 2048 18 / 21.
+  // said): 1 request x 64 nodes, 512 positions 10 / 18, 1024 13 / 21, 2048 18.4 /
+  // 21.4, 2450 21.1 / 21.5, 2700 22.7 / 21.6, 3300 25 / 23.5, 4096 32 / 26 (bf16 1100
+  // 16 / 20, 1500 19.2 / 19.9, 2048 24 / 22); 40 nodes 2048 17.8 / 20.7, 2450 20.5 /
+  // 20.6; 2 x 64 x 2048 20 / 25; 4 x 64 x 700 21.5 / 21.8, 960 24.5 / 23.4, 1500 31 /
+  // 29, 8 x 64 x 1024 48 / 36; 4 x 16 x 2048 20 / 23; single tokens: 1 x 512 8 / 10,
+  // 1 x 2048 18 / 10, 8 x 800 10.8 / 11.6, 8 x 2048 18 / 16, 16 x 2048 18.5 / 20.6,
+  // 32 x 800 14 / 18, 2048 25 / 31.
   const int64_t turns = ((int64_t(max_ctx) + budget + 255) / 256) * (eight ? 1 : 2), few = tiles_of(16);
   // At most 64 items of 16 rows over middle contexts: shared out as for few rows
   // (us, 1 request, 32 / 8 heads, whole or tiles of 64 rows / this way): 8 nodes,
