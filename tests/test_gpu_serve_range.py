@@ -115,3 +115,33 @@ def test_large_numbers_beside_an_infinity():
     want[3, :9] = held(rest[None])[0, :9]              # a NaN alone changes nothing else
     for o in out:
         assert np.array_equal(o.double().cpu().numpy()[0, :, 0], want, equal_nan=True)
+
+
+@pytest.mark.parametrize("kind", [E8, BF])
+@pytest.mark.parametrize("n,ctx,hq,hkv,b", KERNELS)
+def test_a_nan_in_the_context(kind, n, ctx, hq, hkv, b):
+    """A position whose value has a NaN in one element: that element of every row is one, all others keep their bits."""
+    rng = np.random.default_rng(n + 1)
+    dev, page = device(), 16
+    per = (ctx + page - 1) // page
+    p = D.CacheParams(b, hkv, 128, page, b * per, per, kind)
+    x = torch.from_numpy(S.bf16(rng.normal(size=(b, ctx, hkv, 128)))).to(dev).bfloat16()
+    q = torch.from_numpy(S.bf16(rng.normal(size=(b, n, hq, 128)))).to(dev).bfloat16()
+    t = torch.from_numpy(S.bf16(rng.normal(size=(b, n, hkv, 128)))).to(dev).bfloat16()
+    c = make_cache(p, rng.permutation(b * per).reshape(b, per))
+    a = D.AttnParams(b, n, ctx, hq, hkv, 128, 0.0884)
+    need = D.tree_attention_paged_workspace_size(a, p)
+    ws = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
+    outs = []
+    for value in (0.0, float("nan")):
+        v = x.clone()
+        v[:, ctx // 2, :, 70] = value
+        D.cache_write(p, c, x, v, ctx)
+        out = torch.zeros(b, n, hq, 128, dtype=torch.bfloat16, device=dev)
+        say(f"tree_attention_paged, a NaN in the context: b={b} B={n} ctx={ctx} heads={hq}/{hkv} type={kind}")
+        D.tree_attention_paged(a, p, c, q, t, t, None, None, out, ws)
+        torch.cuda.synchronize()
+        outs.append(out.cpu())
+    assert outs[0].isfinite().all() and outs[1][..., 70].isnan().all()
+    outs[1][..., 70] = outs[0][..., 70]
+    assert torch.equal(outs[0].view(torch.int16), outs[1].view(torch.int16))
