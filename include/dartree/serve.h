@@ -26,8 +26,10 @@ extern "C" {
 
 typedef enum dartree_cache_type {
   DARTREE_CACHE_BF16 = 0, /* keys and values as given */
-  DARTREE_CACHE_E4M3 = 1  /* 8 bits (OCP e4m3: 4 exponent bits, 3 of mantissa, largest 448) and one power of
+  DARTREE_CACHE_E4M3 = 1, /* 8 bits (OCP e4m3: 4 exponent bits, 3 of mantissa, largest 448) and one power of
                              two per position, head and side */
+  DARTREE_CACHE_E2M1 = 4  /* 4 bits (OCP e2m1: 2 exponent bits, 1 of mantissa: 0, 0.5, 1, 1.5, 2, 3, 4, 6) and one
+                             power of two per 32 elements of a row */
 } dartree_cache_type;
 
 /* Shape of a cache (host struct). */
@@ -46,10 +48,10 @@ typedef struct dartree_cache_params {
  * page: its positions are dropped by a write, read as zeros and are not seen
  * by attention. */
 typedef struct dartree_cache {
-  void* k;              /* [num_pages][heads_kv][page][128], bf16 or e4m3 */
-  void* v;
-  uint8_t* k_exp;       /* E4M3: [num_pages][heads_kv][page], a row stands for its values * 2^(exp - 127); */
-  uint8_t* v_exp;       /* BF16: not used, may be NULL */
+  void* k;              /* [num_pages][heads_kv][page][128], bf16, e4m3 or e2m1 (64 bytes a row, element 2 i in */
+  void* v;              /* the low half of byte i) */
+  uint8_t* k_exp;       /* E4M3: [num_pages][heads_kv][page], a row stands for its values * 2^(exp - 127); E2M1: */
+  uint8_t* v_exp;       /* [num_pages][heads_kv][page][4], likewise each 32 elements; BF16: not used, may be NULL */
   const int32_t* table; /* [b][max_pages] */
 } dartree_cache;
 
@@ -73,6 +75,11 @@ dartree_status dartree_cache_validate(const dartree_cache_params* p);
  * held above 224, the least normal number is 2^-6).
  * A NaN stays one; an infinity becomes one, and the other values of its row 0.
  *
+ * E2M1: 32 elements are held as e2m1(x * 2^-e), nearest, ties to the even code, with
+ * the least e of -100 .. 125 for which the largest magnitude is at most 6 * 2^e;
+ * exp = e + 127.  Numbers above 6 * 2^125 (2.55e38) are held as that.  32 elements
+ * with a NaN or an infinity are all NaN (exp 255).
+ *
  * Within a call, no two (request, position) pairs may share a slot.  Slots
  * that are not written keep their contents. */
 dartree_status dartree_cache_write(const dartree_cache_params* p, const dartree_cache* cache, int32_t source_rows,
@@ -84,7 +91,8 @@ dartree_status dartree_cache_write(const dartree_cache_params* p, const dartree_
  * request q is position start[q] + i for i < counts[q] (NULL as above), the
  * layout dartree_tree_attention takes its context in.  Exact: e4m3 times a
  * power of two fits bf16, but for +-2^128: the numbers from 248 * 2^120 (3.30e38)
- * on are held as that, and are read as bf16's largest, 255 * 2^120.  Positions
+ * on are held as that, and are read as bf16's largest, 255 * 2^120.  E2M1: exact
+ * for what a write leaves (exp 27 .. 252, or 255 for NaN).  Positions
  * without a page are zeros; rows at and past counts[q] are left as they were. */
 dartree_status dartree_cache_read(const dartree_cache_params* p, const dartree_cache* cache, int32_t rows, void* k,
                                   void* v, const int32_t* counts, const int32_t* start, hipStream_t stream);
@@ -112,7 +120,7 @@ dartree_status dartree_tree_attention_paged_workspace_size(const dartree_attn_pa
  * q: bf16, node i of request r at (r * budget + i) * q_stride elements,
  * heads_q * 128 each; k_tree, v_tree: likewise with kv_stride and heads_kv;
  * strides are multiples of 8.  out: bf16 [b][budget][heads_q][128].
- * Products of bf16 values (e4m3 keys and values as dartree_cache_read gives
+ * Products of bf16 values (e4m3 and e2m1 keys and values as dartree_cache_read gives
  * them) with fp32 accumulation, fp32 softmax; the weights are rounded to bf16 for
  * the weighted sum of values, the output to bf16.  Weights are at most 2^8 before
  * they are divided by their sum: values below 2^89 cannot overflow it.  The order

@@ -1,10 +1,11 @@
 // The paged key/value cache: rows of 128 bf16 elements written to pages, as
-// they are or in e4m3 with one power of two per row, and read back.
+// they are, in e4m3 with one power of two per row or in e2m1 with one per 32
+// elements, and read back.
 //
-// A row is 16 lanes of 8 elements (16 bytes of bf16, 8 of e4m3); a lane moves
+// A row is 16 lanes of 8 elements (16 bytes of bf16, 8 of e4m3, 4 of e2m1); a lane moves
 // its eighth of the key and of the value row of one (request, position, head),
 // heads fastest, so that a wave reads 1 KB of consecutive source bytes and
-// writes whole 128- or 256-byte rows.  A power of two as scale costs nothing:
+// writes whole rows of 256, 128 or 64 bytes.  A power of two as scale costs nothing:
 // e4m3 is a floating type, its rounding is relative, and scaling by a power of
 // two is exact, so the bytes are the nearest ones to x 2^-e whatever the order
 // of operations.
@@ -14,7 +15,6 @@
 namespace dartree {
 namespace {
 
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 // Slot of position `pos` of request q: its index among all (page, slot) pairs
@@ -35,6 +35,42 @@ __device__ __forceinline__ int row_exponent(float amax) {
 
 __device__ __forceinline__ float low(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float high(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
+
+// Least e >= kExpLow with amax <= 6 * 2^e = 1.5 * 2^(e + 2).  At most 125: 6 * 2^126
+// is no bf16 number, so the numbers above 6 * 2^125 are held as that.
+__device__ __forceinline__ int block_exponent(float amax) {
+  const uint32_t u = __float_as_uint(amax);
+  const int e = int(u >> 23) - 127 - 2 + ((u & 0x7FFFFFu) > 0x400000u);
+  return min(max(e, kExpLow), 125);
+}
+
+// Eight elements of a row to e2m1, the first in the lowest bits, and the exponent
+// byte of their block, which four lanes hold.  The conversion divides by its scale,
+// rounds to the nearest, ties to the even code, and takes what is above 6 as 6.  A
+// NaN or an infinity has no e2m1 code: the whole block counts as NaN (byte 255).
+__device__ __forceinline__ uint32_t quantise4(u32x4 x, uint32_t& byte) {
+  float f[8], m = 0.f;
+  bool odd = false;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    f[2 * i] = low(x[i]);
+    f[2 * i + 1] = high(x[i]);
+    m = fmaxf(m, fmaxf(fabsf(f[2 * i]), fabsf(f[2 * i + 1])));
+    odd |= (x[i] & 0x7F80u) == 0x7F80u || (x[i] & 0x7F800000u) == 0x7F800000u;
+  }
+  if (odd) m = INFINITY;
+  m = fmaxf(m, __shfl_xor(m, 1));
+  m = fmaxf(m, __shfl_xor(m, 2));
+  const int e = block_exponent(m);
+  const float s = __uint_as_float(uint32_t(127 + e) << 23);
+  uint32_t out = 0;
+  out = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(out, f[0], f[1], s, 0);
+  out = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(out, f[2], f[3], s, 1);
+  out = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(out, f[4], f[5], s, 2);
+  out = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(out, f[6], f[7], s, 3);
+  byte = m == INFINITY ? 255u : uint32_t(e + 127);
+  return m == INFINITY ? 0u : out;
+}
 
 // Eight elements of a row (16 lanes hold it) to e4m3; the row's exponent in e.
 __device__ __forceinline__ u32x2 quantise(u32x4 x, int& e) {
@@ -59,7 +95,7 @@ __device__ __forceinline__ u32x2 quantise(u32x4 x, int& e) {
   return out;
 }
 
-template <bool E8>
+template <int BITS>
 __global__ __launch_bounds__(256) void cache_write(CacheMoveArgs a) {
   const unsigned r = blockIdx.x * 16 + (threadIdx.x >> 4);   // below 2^31
   const int lane = threadIdx.x & 15;
@@ -76,13 +112,21 @@ __global__ __launch_bounds__(256) void cache_write(CacheMoveArgs a) {
   const u32x4 v = *reinterpret_cast<const u32x4*>(a.v_in + at);
   const int64_t row = slot + (int64_t(head) << a.c.page_log2);
   const int64_t to = row * kHead + lane * 8;
-  if (E8) {
+  if constexpr (BITS == 8) {
     int ek, ev;
     *reinterpret_cast<u32x2*>(static_cast<uint8_t*>(a.c.k) + to) = quantise(k, ek);
     *reinterpret_cast<u32x2*>(static_cast<uint8_t*>(a.c.v) + to) = quantise(v, ev);
     if (lane == 0) {
       a.c.k_exp[row] = uint8_t(ek + 127);
       a.c.v_exp[row] = uint8_t(ev + 127);
+    }
+  } else if constexpr (BITS == 4) {
+    uint32_t ek, ev;
+    *reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(a.c.k) + to / 2) = quantise4(k, ek);
+    *reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(a.c.v) + to / 2) = quantise4(v, ev);
+    if ((lane & 3) == 0) {
+      a.c.k_exp[row * (kHead / kBlock) + (lane >> 2)] = uint8_t(ek);
+      a.c.v_exp[row * (kHead / kBlock) + (lane >> 2)] = uint8_t(ev);
     }
   } else {
     *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(a.c.k) + to) = k;
@@ -102,7 +146,7 @@ __device__ __forceinline__ u32x4 expand(u32x2 x, uint32_t e) {
   return out;
 }
 
-template <bool E8>
+template <int BITS>
 __global__ __launch_bounds__(256) void cache_read(CacheMoveArgs a) {
   const unsigned r = blockIdx.x * 16 + (threadIdx.x >> 4);   // below 2^31
   const int lane = threadIdx.x & 15;
@@ -116,7 +160,7 @@ __global__ __launch_bounds__(256) void cache_read(CacheMoveArgs a) {
   if (slot >= 0) {
     const int64_t row = slot + (int64_t(head) << a.c.page_log2);
     const int64_t from = row * kHead + lane * 8;
-    if (E8) {
+    if constexpr (BITS == 8) {
       const u32x2 xk = *reinterpret_cast<const u32x2*>(static_cast<const uint8_t*>(a.c.k) + from);
       const u32x2 xv = *reinterpret_cast<const u32x2*>(static_cast<const uint8_t*>(a.c.v) + from);
       const uint32_t ek = a.c.k_exp[row], ev = a.c.v_exp[row];
@@ -129,6 +173,12 @@ __global__ __launch_bounds__(256) void cache_read(CacheMoveArgs a) {
           v[i] = finite_pair(v[i]);
         }
       }
+    } else if constexpr (BITS == 4) {
+      const uint32_t xk = *reinterpret_cast<const uint32_t*>(static_cast<const uint8_t*>(a.c.k) + from / 2);
+      const uint32_t xv = *reinterpret_cast<const uint32_t*>(static_cast<const uint8_t*>(a.c.v) + from / 2);
+      const int64_t block = row * (kHead / kBlock) + (lane >> 2);
+      k = expand8(xk, __uint_as_float(uint32_t(a.c.k_exp[block]) << 23));
+      v = expand8(xv, __uint_as_float(uint32_t(a.c.v_exp[block]) << 23));
     } else {
       k = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(a.c.k) + from);
       v = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(a.c.v) + from);
@@ -146,14 +196,14 @@ unsigned blocks_of(const CacheMoveArgs& a) {
 }  // namespace
 
 hipError_t launch_cache_write(const CacheMoveArgs& a, hipStream_t s) {
-  if (a.eight) hipLaunchKernelGGL(cache_write<true>, dim3(blocks_of(a)), dim3(256), 0, s, a);
-  else hipLaunchKernelGGL(cache_write<false>, dim3(blocks_of(a)), dim3(256), 0, s, a);
+  auto* kernel = a.bits == 4 ? cache_write<4> : a.bits == 8 ? cache_write<8> : cache_write<16>;
+  hipLaunchKernelGGL(kernel, dim3(blocks_of(a)), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 
 hipError_t launch_cache_read(const CacheMoveArgs& a, hipStream_t s) {
-  if (a.eight) hipLaunchKernelGGL(cache_read<true>, dim3(blocks_of(a)), dim3(256), 0, s, a);
-  else hipLaunchKernelGGL(cache_read<false>, dim3(blocks_of(a)), dim3(256), 0, s, a);
+  auto* kernel = a.bits == 4 ? cache_read<4> : a.bits == 8 ? cache_read<8> : cache_read<16>;
+  hipLaunchKernelGGL(kernel, dim3(blocks_of(a)), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 

@@ -23,6 +23,7 @@
 //
 // More rows (paged_tiles): below.
 #include <algorithm>
+#include <type_traits>
 
 #include "reduce.hpp"
 #include "serve.hpp"
@@ -30,7 +31,6 @@
 namespace dartree {
 namespace {
 
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kChunk = 32;            // keys of a wave's share of a step
@@ -183,25 +183,29 @@ struct Index {
   static constexpr int value = N;
 };
 
-template <bool E8>
+template <int BITS>
 struct Chunk {   // 32 keys and values as read
-  u32x4 k[2][E8 ? 2 : 4];
-  u32x2 v8[E8 ? 8 : 1];
-  u32x4 v16[E8 ? 1 : 8];
+  u32x4 k[2][BITS / 4];
+  uint32_t v4[BITS == 4 ? 8 : 1];
+  u32x2 v8[BITS == 8 ? 8 : 1];
+  u32x4 v16[BITS == 16 ? 8 : 1];
   uint32_t ke[2];
-  u32x2 ve;
+  u32x2 ve;      // e4m3: exponent bytes of keys 4 g .. + 3 of both tiles
+  u32x4 vb[2];   // e2m1: of their four blocks each
 };
 
 // Scores of a chunk.  TOP: keys' exponents may be kTopByte and more.
-template <bool E8, bool TOP>
-__device__ __forceinline__ void chunk_scores(const Chunk<E8>& c, const u32x4 (&qf)[4], f32x4 (&s)[2]) {
+template <int BITS, bool TOP>
+__device__ __forceinline__ void chunk_scores(const Chunk<BITS>& c, const u32x4 (&qf)[4], f32x4 (&s)[2]) {
 #pragma unroll
   for (int t = 0; t < 2; ++t) {
     s[t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int ks = 0; ks < 4; ++ks) {
       u32x4 kf;
-      if constexpr (E8) {
+      if constexpr (BITS == 4) {
+        kf = expand8(c.k[t][0][ks], __uint_as_float(c.ke[t] << 23));
+      } else if constexpr (BITS == 8) {
         const float sc = __uint_as_float(uint32_t(c.ke[t]) << 23);
         const uint32_t w0 = c.k[t][ks >> 1][2 * (ks & 1)], w1 = c.k[t][ks >> 1][2 * (ks & 1) + 1];
         kf = u32x4{expand2<false>(w0, sc), expand2<true>(w0, sc), expand2<false>(w1, sc), expand2<true>(w1, sc)};
@@ -257,17 +261,28 @@ __device__ __forceinline__ void chunk_weights(f32x4 (&s)[2], const bool masked, 
 
 // O of a chunk.  V: dims 8 c + 2 j, 8 c + 2 j + 1 of eight keys, transposed.  A key
 // that is not there has zeros instead of what its memory holds: 0 * NaN is NaN.
-template <bool E8, bool TOP>
-__device__ __forceinline__ void chunk_values(const Chunk<E8>& c, const uint32_t there, const u32x4& p, Rows& st) {
+template <int BITS, bool TOP>
+__device__ __forceinline__ void chunk_values(const Chunk<BITS>& c, const uint32_t there, const u32x4& p, Rows& st) {
   const int g = (threadIdx.x & 63) >> 4;
   const uint32_t here = there >> (4 * g);
   const bool whole = there == ~0u;
+  u32x4 x4[BITS == 4 ? 8 : 1];
+  if constexpr (BITS == 4) {   // dims 8 c .. 8 c + 7 lie in block c / 4; its byte to the exponent's place
+    const int turn = (8 * ((threadIdx.x & 15) >> 2) + 9) & 31;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const uint32_t word = c.vb[e >> 2][e & 3];
+      x4[e] = expand8(c.v4[e], __uint_as_float(__builtin_amdgcn_alignbit(word, word, turn)));
+    }
+  }
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     uint32_t w[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      if constexpr (E8) {
+      if constexpr (BITS == 4) {
+        w[e] = x4[e][j];
+      } else if constexpr (BITS == 8) {
         const uint32_t byte = (c.ve[e >> 2] >> (8 * (e & 3))) & 0xFFu;
         const float sc = __uint_as_float(byte << 23);
         w[e] = (j & 1) ? expand2<true>(c.v8[e][j >> 1], sc) : expand2<false>(c.v8[e][j >> 1], sc);
@@ -302,7 +317,7 @@ __device__ __forceinline__ Parts parts_of(const PagedArgs& a, int blocks) {
   return Parts{o, o + int64_t(blocks) * 2 * ROWS * kHead};
 }
 
-template <bool E8, int W>
+template <int BITS, int W>
 __global__ __launch_bounds__(64 * W, 8 / W) void paged_attention(PagedArgs a, int whole) {
   constexpr int kWaves = W, kStep = kChunk * W;
   __shared__ __attribute__((aligned(16))) float red[kWaves * 8 * 64 * 4];
@@ -330,10 +345,10 @@ __global__ __launch_bounds__(64 * W, 8 / W) void paged_attention(PagedArgs a, in
     const int row = min(rt * 16 + c16, rows - 1);   // past the end: the last row, never stored
     const int node = row / a.group;
     const int64_t from = (int64_t(q) * a.budget + node) * a.q_stride + (kvh * a.group + row - node * a.group) * kHead;
-    // operand ks: dims 64 (ks / 2) + 16 g + 8 (ks % 2) .. + 7, for keys alike
+    // operand ks: eight dims from here on, for keys alike (e2m1: a lane's dims are one block)
+    auto dim_of = [&](int ks) { return BITS == 4 ? 32 * g + 8 * ks : 64 * (ks >> 1) + 16 * g + 8 * (ks & 1); };
 #pragma unroll
-    for (int ks = 0; ks < 4; ++ks)
-      qf[ks] = *reinterpret_cast<const u32x4*>(a.q + from + 64 * (ks >> 1) + 16 * g + 8 * (ks & 1));
+    for (int ks = 0; ks < 4; ++ks) qf[ks] = *reinterpret_cast<const u32x4*>(a.q + from + dim_of(ks));
     const uint32_t* mrow = a.mask ? reinterpret_cast<const uint32_t*>(a.mask) + (int64_t(q) * a.budget + node) * words : nullptr;
     clear(st);
 
@@ -344,7 +359,7 @@ __global__ __launch_bounds__(64 * W, 8 / W) void paged_attention(PagedArgs a, in
     const int kb0 = step * kStep + wave * kChunk;
     const int chunks = kb0 < ex.ctx ? min(min(step + n, nctx) - step, (ex.ctx - kb0 + kStep - 1) / kStep) : 0;
     if (chunks > 0) {
-      Chunk<E8> ch;
+      Chunk<BITS> ch;
       f32x4 sc[2];
       u32x4 p;
       int p0, p1;   // pages of the halves of the chunk to fetch next
@@ -354,7 +369,8 @@ __global__ __launch_bounds__(64 * W, 8 / W) void paged_attention(PagedArgs a, in
       };
       int64_t row0[2] = {0, 0};   // the tiles' first rows
       uint32_t next = 0;          // which keys of the fetched chunk are there
-      const int koff = E8 ? c16 * kHead + 16 * g : c16 * 2 * kHead + 32 * g, voff = E8 ? 4 * g * kHead + 8 * c16 : 4 * g * 2 * kHead + 16 * c16;
+      constexpr int kRow = kHead * BITS / 8;   // bytes
+      const int koff = c16 * kRow + (BITS == 16 ? 32 : 16) * g, voff = 4 * g * kRow + BITS * c16;
       auto fetch_keys = [&](int kb) __attribute__((always_inline)) {
         const int valid = min(kChunk, ex.ctx - kb);
         next = valid == 32 ? ~0u : (1u << valid) - 1u;
@@ -366,8 +382,11 @@ __global__ __launch_bounds__(64 * W, 8 / W) void paged_attention(PagedArgs a, in
         row0[1] = ((h1 * a.heads_kv + kvh) << a.c.page_log2) + ((kb + 16) & (page_size - 1));
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-          const char* kp = static_cast<const char*>(a.c.k) + row0[t] * (E8 ? kHead : 2 * kHead);
-          if constexpr (E8) {
+          const char* kp = static_cast<const char*>(a.c.k) + row0[t] * kRow;
+          if constexpr (BITS == 4) {
+            ch.k[t][0] = *reinterpret_cast<const u32x4*>(kp + koff);
+            ch.ke[t] = (a.c.k_exp + row0[t] * (kHead / kBlock))[4 * c16 + g];
+          } else if constexpr (BITS == 8) {
             ch.k[t][0] = *reinterpret_cast<const u32x4*>(kp + koff);
             ch.k[t][1] = *reinterpret_cast<const u32x4*>(kp + koff + 64);
             ch.ke[t] = (a.c.k_exp + row0[t])[c16];
@@ -381,11 +400,17 @@ __global__ __launch_bounds__(64 * W, 8 / W) void paged_attention(PagedArgs a, in
       auto fetch_values = [&] __attribute__((always_inline)) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          const char* vp = static_cast<const char*>(a.c.v) + row0[e >> 2] * (E8 ? kHead : 2 * kHead);
-          if constexpr (E8) ch.v8[e] = *reinterpret_cast<const u32x2*>(vp + voff + (e & 3) * kHead);
-          else ch.v16[e] = *reinterpret_cast<const u32x4*>(vp + voff + (e & 3) * 2 * kHead);
+          const char* vp = static_cast<const char*>(a.c.v) + row0[e >> 2] * kRow + voff + (e & 3) * kRow;
+          if constexpr (BITS == 4) ch.v4[e] = *reinterpret_cast<const uint32_t*>(vp);
+          else if constexpr (BITS == 8) ch.v8[e] = *reinterpret_cast<const u32x2*>(vp);
+          else ch.v16[e] = *reinterpret_cast<const u32x4*>(vp);
         }
-        if constexpr (E8) {
+        if constexpr (BITS == 4) {
+#pragma unroll
+          for (int t = 0; t < 2; ++t)
+            ch.vb[t] = *reinterpret_cast<const u32x4*>(a.c.v_exp + row0[t] * (kHead / kBlock) + 16 * g);
+        }
+        if constexpr (BITS == 8) {
 #pragma unroll
           for (int t = 0; t < 2; ++t) ch.ve[t] = *reinterpret_cast<const uint32_t*>(a.c.v_exp + row0[t] + 4 * g);
         }
@@ -401,10 +426,10 @@ __global__ __launch_bounds__(64 * W, 8 / W) void paged_attention(PagedArgs a, in
           const int kb = kb0 + (i + 1) * kStep;
           const bool more = i + 1 < chunks;
           if (more) look_up(kb);
-          chunk_scores<E8, TOP.value>(ch, qf, sc);
-          uint32_t e0 = E8 ? ch.ke[0] : 0, e1 = E8 ? ch.ke[1] : 0;
+          chunk_scores<BITS, TOP.value>(ch, qf, sc);
+          uint32_t e0 = BITS == 8 ? ch.ke[0] : 0, e1 = BITS == 8 ? ch.ke[1] : 0;
           if (more) fetch_keys(kb);
-          if constexpr (E8 && !TOP.value) {
+          if constexpr (BITS == 8 && !TOP.value) {
             if (there != ~0u) {
               if (!((there >> c16) & 1u)) e0 = 0;
               if (!((there >> (16 + c16)) & 1u)) e1 = 0;
@@ -412,12 +437,12 @@ __global__ __launch_bounds__(64 * W, 8 / W) void paged_attention(PagedArgs a, in
             most = max(most, max(e0, e1));
           }
           chunk_weights(sc, there != ~0u, there, a.scale_log2, st, p);
-          chunk_values<E8, TOP.value>(ch, there, p, st);
+          chunk_values<BITS, TOP.value>(ch, there, p, st);
           if (more) fetch_values();
         }
       };
       walk(Index<false>());
-      if constexpr (E8) {
+      if constexpr (BITS == 8) {
         // Rows with a key of kTopByte and more, and values that gave something else than
         // a finite sum (as the infinities of such exponents do): once more, converted
         // with care.  Tests in the loop cost 5 % (1 x 64 nodes x 2048 positions:
@@ -446,13 +471,12 @@ __global__ __launch_bounds__(64 * W, 8 / W) void paged_attention(PagedArgs a, in
       auto at = [&](int key) {
         return (int64_t(q) * a.budget + min(kb + key, ex.nodes - 1)) * a.kv_stride + kvh * kHead;
       };
-      Chunk<false> ch;
+      Chunk<16> ch;
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
-        const uint16_t* kp = a.k_tree + at(16 * t + c16) + 16 * g;
+        const uint16_t* kp = a.k_tree + at(16 * t + c16);
 #pragma unroll
-        for (int ks = 0; ks < 4; ++ks)
-          ch.k[t][ks] = *reinterpret_cast<const u32x4*>(kp + 64 * (ks >> 1) + 8 * (ks & 1));
+        for (int ks = 0; ks < 4; ++ks) ch.k[t][ks] = *reinterpret_cast<const u32x4*>(kp + dim_of(ks));
       }
 #pragma unroll
       for (int e = 0; e < 8; ++e)
@@ -472,9 +496,9 @@ __global__ __launch_bounds__(64 * W, 8 / W) void paged_attention(PagedArgs a, in
       }
       f32x4 sc[2];
       u32x4 p;
-      chunk_scores<false, false>(ch, qf, sc);
+      chunk_scores<16, false>(ch, qf, sc);
       chunk_weights(sc, true, seen & there, a.scale_log2, st, p);
-      chunk_values<false, false>(ch, there, p, st);
+      chunk_values<16, false>(ch, there, p, st);
     }
     if (odd)
       for (int s = max(step, nctx); s < step + n; ++s) {
@@ -583,7 +607,7 @@ __device__ __forceinline__ int thread_again() {
   return t;
 }
 
-template <int RG, bool E8, int W>
+template <int RG, int BITS, int W>
 __global__ __launch_bounds__(64 * W, 8 / W) void paged_tiles(PagedArgs a, int whole) {
   __shared__ __attribute__((aligned(16))) char smem[4 * kTileBytes];   // [buffer][K, V]
   __shared__ int odd;   // the last of the block's items (counted from 1) whose tree holds values that are no numbers
@@ -764,8 +788,9 @@ __global__ __launch_bounds__(64 * W, 8 / W) void paged_tiles(PagedArgs a, int wh
 
     {   // the context
       const int32_t* table = a.c.table + int64_t(q) * a.c.max_pages;
-      constexpr int kRowsWave = E8 ? 8 : 4, kShares = kTile / (kRowsWave * W);
-      u32x4 kx[kShares], vx[kShares];
+      constexpr int kRowsWave = BITS == 16 ? 4 : 8, kShares = kTile / (kRowsWave * W);
+      typedef std::conditional_t<BITS == 4, u32x2, u32x4> Piece;   // of a row, a lane's
+      Piece kx[kShares], vx[kShares];
       uint32_t ke[kShares], ve[kShares];
       uint64_t in_flight = 0;
       int page;   // lane i % 4: the page of the i-th 16 keys of the tile to fetch next
@@ -773,7 +798,7 @@ __global__ __launch_bounds__(64 * W, 8 / W) void paged_tiles(PagedArgs a, int wh
         page = table[min(s * kTile + 16 * (thread_again() & 3), ex.ctx - 1) >> a.c.page_log2];
       };
       // a wave's keys of a share lie in one group of 16, so in one page: eight rows
-      // of 128 bytes in e4m3, four of 256 in bf16, from key first_key(i)
+      // of 128 or 64 bytes, four of 256 in bf16, from key first_key(i)
       auto first_key = [&](int i) { return kRowsWave * (W * i + wave); };
       auto fetch = [&](int s) __attribute__((always_inline)) {
         const int kb = s * kTile, valid = min(kTile, ex.ctx - kb);
@@ -786,10 +811,13 @@ __global__ __launch_bounds__(64 * W, 8 / W) void paged_tiles(PagedArgs a, int wh
           const int of = __builtin_amdgcn_readlane(page, first_key(i) >> 4);
           const int64_t in = uint32_t(of) < uint32_t(a.c.num_pages) ? of : 0;   // any page: what is read is not used
           const int64_t row0 = ((in * a.heads_kv + kvh) << a.c.page_log2) + ((kb + first_key(i)) & page_mask);
-          const int64_t byte0 = row0 * (E8 ? kHead : 2 * kHead);
-          kx[i] = *reinterpret_cast<const u32x4*>(static_cast<const char*>(a.c.k) + byte0 + 16 * lane);
-          vx[i] = *reinterpret_cast<const u32x4*>(static_cast<const char*>(a.c.v) + byte0 + 16 * lane);
-          if constexpr (E8) {
+          const int64_t byte0 = row0 * (kHead * BITS / 8) + int64_t(sizeof(Piece)) * lane;
+          kx[i] = *reinterpret_cast<const Piece*>(static_cast<const char*>(a.c.k) + byte0);
+          vx[i] = *reinterpret_cast<const Piece*>(static_cast<const char*>(a.c.v) + byte0);
+          if constexpr (BITS == 4) {   // a lane's 16 elements lie in one block
+            ke[i] = a.c.k_exp[row0 * (kHead / kBlock) + (lane >> 1)];
+            ve[i] = a.c.v_exp[row0 * (kHead / kBlock) + (lane >> 1)];
+          } else if constexpr (BITS == 8) {
             ke[i] = a.c.k_exp[row0 + (lane >> 3)];
             ve[i] = a.c.v_exp[row0 + (lane >> 3)];
           }
@@ -798,14 +826,22 @@ __global__ __launch_bounds__(64 * W, 8 / W) void paged_tiles(PagedArgs a, int wh
       };
       auto store = [&](auto B) __attribute__((always_inline)) -> uint64_t {
         const uint64_t there = in_flight;
-        const u32x4 zero{0, 0, 0, 0};
+        const Piece zero = {};
         LDS_AS char* const kt = lds + B.value * 2 * kTileBytes;
 #pragma unroll
         for (int i = 0; i < kShares; ++i) {
-          const int key = first_key(i) + (E8 ? lane >> 3 : g);
+          const int key = first_key(i) + (BITS == 16 ? g : lane >> 3);
           const bool gone = there != ~0ull && !((there >> key) & 1);
           if (gone) vx[i] = zero;
-          if constexpr (E8) {
+          if constexpr (BITS == 4) {
+            const float sk = __uint_as_float(ke[i] << 23), sv = gone ? 1.f : __uint_as_float(ve[i] << 23);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              const int c = 2 * (lane & 7) + h;
+              *reinterpret_cast<LDS_AS u32x4*>(kt + key * kRowBytes + (c ^ k_place(key)) * 16) = expand8(kx[i][h], sk);
+              *reinterpret_cast<LDS_AS u32x4*>(kt + kTileBytes + key * kRowBytes + (c ^ v_place(key)) * 16) = expand8(vx[i][h], sv);
+            }
+          } else if constexpr (BITS == 8) {
             const float sk = __uint_as_float(ke[i] << 23), sv = gone ? 1.f : __uint_as_float(ve[i] << 23);
             u32x4 k[2], v[2];
 #pragma unroll
@@ -1074,7 +1110,7 @@ struct Plan {
   int rows, blocks, whole;
   int64_t items;
 };
-Plan plan_of(int batch, int budget, int max_ctx, int heads_q, int heads_kv, int eight) {
+Plan plan_of(int batch, int budget, int max_ctx, int heads_q, int heads_kv, int bits) {
   constexpr int kResident = 512;   // two blocks of four waves a compute unit
   const int rows = budget * (heads_q / heads_kv);
   const int64_t heads = int64_t(batch) * heads_kv;
@@ -1090,7 +1126,7 @@ Plan plan_of(int batch, int budget, int max_ctx, int heads_q, int heads_kv, int 
   // 29, 8 x 64 x 1024 48 / 36; 4 x 16 x 2048 20 / 23; single tokens: 1 x 512 8 / 10,
   // 1 x 2048 18 / 10, 8 x 800 10.8 / 11.6, 8 x 2048 18 / 16, 16 x 2048 18.5 / 20.6,
   // 32 x 800 14 / 18, 2048 25 / 31.
-  const int64_t turns = ((int64_t(max_ctx) + budget + 255) / 256) * (eight ? 1 : 2), few = tiles_of(16);
+  const int64_t turns = ((int64_t(max_ctx) + budget + 255) / 256) * (bits == 16 ? 2 : 1), few = tiles_of(16);
   // At most 64 items of 16 rows over middle contexts: shared out as for few rows
   // (us, 1 request, 32 / 8 heads, whole or tiles of 64 rows / this way): 8 nodes,
   // 1280 positions 12.8 / 10.7, 2048 16.9 / 12.1, 16000 22.1 / 18.9, 32768 in bf16
@@ -1148,27 +1184,32 @@ hipError_t launch(K* kernel, const PagedArgs& a, const Plan& p, hipStream_t s) {
   return hipGetLastError();
 }
 
+template <int BITS>
+hipError_t launch_kernel(const PagedArgs& a, const Plan& p, hipStream_t s) {
+  switch (p.kernel) {
+    case kFew:
+      return launch<16, 128>(paged_attention<BITS, 4>, a, p, s);
+    case kFewWhole:
+      return launch_whole(paged_attention<BITS, 8>, 512, a, p, s);
+    case kTiles64:
+      return launch<64, kTile>(paged_tiles<1, BITS, 4>, a, p, s);
+    case kTiles128:
+      return launch<128, kTile>(paged_tiles<2, BITS, 4>, a, p, s);
+    default:
+      return launch_whole(paged_tiles<2, BITS, 8>, 512, a, p, s);
+  }
+}
+
 }  // namespace
 
-size_t paged_attention_workspace(int batch, int budget, int max_ctx, int heads_q, int heads_kv, int eight) {
-  const Plan p = plan_of(batch, budget, max_ctx, heads_q, heads_kv, eight);
+size_t paged_attention_workspace(int batch, int budget, int max_ctx, int heads_q, int heads_kv, int bits) {
+  const Plan p = plan_of(batch, budget, max_ctx, heads_q, heads_kv, bits);
   return p.whole ? 0 : size_t(p.blocks) * 2 * p.rows * (kHead + 2) * sizeof(float);
 }
 
 hipError_t launch_paged_attention(const PagedArgs& a, hipStream_t s) {
-  const Plan p = plan_of(a.batch, a.budget, a.max_ctx, a.heads_q, a.heads_kv, a.eight);
-  switch (p.kernel) {
-    case kFew:
-      return a.eight ? launch<16, 128>(paged_attention<true, 4>, a, p, s) : launch<16, 128>(paged_attention<false, 4>, a, p, s);
-    case kFewWhole:
-      return a.eight ? launch_whole(paged_attention<true, 8>, 512, a, p, s) : launch_whole(paged_attention<false, 8>, 512, a, p, s);
-    case kTiles64:
-      return a.eight ? launch<64, kTile>(paged_tiles<1, true, 4>, a, p, s) : launch<64, kTile>(paged_tiles<1, false, 4>, a, p, s);
-    case kTiles128:
-      return a.eight ? launch<128, kTile>(paged_tiles<2, true, 4>, a, p, s) : launch<128, kTile>(paged_tiles<2, false, 4>, a, p, s);
-    default:
-      return a.eight ? launch_whole(paged_tiles<2, true, 8>, 512, a, p, s) : launch_whole(paged_tiles<2, false, 8>, 512, a, p, s);
-  }
+  const Plan p = plan_of(a.batch, a.budget, a.max_ctx, a.heads_q, a.heads_kv, a.bits);
+  return a.bits == 4 ? launch_kernel<4>(a, p, s) : a.bits == 8 ? launch_kernel<8>(a, p, s) : launch_kernel<16>(a, p, s);
 }
 
 }  // namespace dartree

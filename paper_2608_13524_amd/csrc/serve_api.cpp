@@ -15,7 +15,8 @@ dartree_status check_cache(const dartree_cache_params* p) {
   if (!p) return DARTREE_ERR_INVALID_ARG;
   if (p->batch < 1 || p->heads_kv < 1 || p->head_dim < 1 || p->page < 1 || p->num_pages < 1 || p->max_pages < 1)
     return DARTREE_ERR_INVALID_ARG;
-  if (p->type != DARTREE_CACHE_BF16 && p->type != DARTREE_CACHE_E4M3) return DARTREE_ERR_INVALID_ARG;
+  if (p->type != DARTREE_CACHE_BF16 && p->type != DARTREE_CACHE_E4M3 && p->type != DARTREE_CACHE_E2M1)
+    return DARTREE_ERR_INVALID_ARG;
   if (p->head_dim != kHead || p->heads_kv > 4096) return DARTREE_ERR_UNSUPPORTED;
   if (p->page < 16 || p->page > 256 || (p->page & (p->page - 1)) != 0) return DARTREE_ERR_UNSUPPORTED;
   if (int64_t(p->max_pages) * p->page > (int64_t(1) << 30)) return DARTREE_ERR_UNSUPPORTED;
@@ -24,8 +25,12 @@ dartree_status check_cache(const dartree_cache_params* p) {
 
 dartree_status check_memory(const dartree_cache_params& p, const dartree_cache* c) {
   if (!c || !given(c->k) || !given(c->v) || !given(c->table)) return DARTREE_ERR_INVALID_ARG;
-  if (p.type == DARTREE_CACHE_E4M3 && (!given(c->k_exp) || !given(c->v_exp))) return DARTREE_ERR_INVALID_ARG;
+  if (p.type != DARTREE_CACHE_BF16 && (!given(c->k_exp) || !given(c->v_exp))) return DARTREE_ERR_INVALID_ARG;
   return DARTREE_OK;
+}
+
+int bits_of(const dartree_cache_params& p) {
+  return p.type == DARTREE_CACHE_BF16 ? 16 : p.type == DARTREE_CACHE_E4M3 ? 8 : 4;
 }
 
 CacheView view_of(const dartree_cache_params& p, const dartree_cache& c) {
@@ -101,7 +106,7 @@ dartree_status dartree_cache_write(const dartree_cache_params* p, const dartree_
   if (!stride_ok(row_stride, int64_t(p->heads_kv) * kHead)) return DARTREE_ERR_INVALID_ARG;
   CacheMoveArgs a{};
   a.c = view_of(*p, *cache);
-  a.eight = p->type == DARTREE_CACHE_E4M3;
+  a.bits = bits_of(*p);
   a.source_rows = source_rows;
   a.rows = rows;
   a.k_in = static_cast<const uint16_t*>(k);
@@ -122,7 +127,7 @@ dartree_status dartree_cache_read(const dartree_cache_params* p, const dartree_c
   if (!given(k) || !given(v) || !optional(counts) || !optional(start)) return DARTREE_ERR_INVALID_ARG;
   CacheMoveArgs a{};
   a.c = view_of(*p, *cache);
-  a.eight = p->type == DARTREE_CACHE_E4M3;
+  a.bits = bits_of(*p);
   a.rows = rows;
   a.k_out = static_cast<uint16_t*>(k);
   a.v_out = static_cast<uint16_t*>(v);
@@ -136,7 +141,7 @@ dartree_status dartree_tree_attention_paged_workspace_size(const dartree_attn_pa
   if (!bytes) return DARTREE_ERR_INVALID_ARG;
   const dartree_status s = check_paged(a, p);
   if (s != DARTREE_OK) return s;
-  *bytes = paged_attention_workspace(a->batch, a->budget, a->max_ctx, a->heads_q, a->heads_kv, p->type == DARTREE_CACHE_E4M3);
+  *bytes = paged_attention_workspace(a->batch, a->budget, a->max_ctx, a->heads_q, a->heads_kv, bits_of(*p));
   return DARTREE_OK;
 }
 
@@ -153,13 +158,13 @@ dartree_status dartree_tree_attention_paged(const dartree_attn_params* a, const 
     return DARTREE_ERR_INVALID_ARG;
   if (!stride_ok(q_stride, int64_t(a->heads_q) * kHead) || !stride_ok(kv_stride, int64_t(a->heads_kv) * kHead))
     return DARTREE_ERR_INVALID_ARG;
-  const int eight = p->type == DARTREE_CACHE_E4M3;
+  const int bits = bits_of(*p);
   if (!workspace_fits(ws, ws_bytes,
-                      paged_attention_workspace(a->batch, a->budget, a->max_ctx, a->heads_q, a->heads_kv, eight)))
+                      paged_attention_workspace(a->batch, a->budget, a->max_ctx, a->heads_q, a->heads_kv, bits)))
     return DARTREE_ERR_WORKSPACE;
   PagedArgs g{};
   g.c = view_of(*p, *cache);
-  g.eight = eight;
+  g.bits = bits;
   g.batch = a->batch;
   g.budget = a->budget;
   g.max_ctx = a->max_ctx;

@@ -20,6 +20,7 @@ HEAD_RNN = 0
 HEAD_MARKOV = 1
 CACHE_BF16 = 0
 CACHE_E4M3 = 1
+CACHE_E2M1 = 4
 
 OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_WORKSPACE, ERR_HIP, ERR_ORDER, ERR_NONFINITE = range(7)
 
@@ -635,8 +636,9 @@ def _on_device(where: str, device: int) -> None:
 
 @dataclasses.dataclass
 class DeviceCache:
-    """Pages k, v [num_pages][heads_kv][page][128] (bfloat16 or float8_e4m3fn),
-    k_exp, v_exp uint8 [num_pages][heads_kv][page] (e4m3 only), table int32
+    """Pages k, v [num_pages][heads_kv][page][128] (bfloat16 or float8_e4m3fn; e2m1:
+    uint8 [..][64], element 2 i in the low half of byte i), k_exp, v_exp uint8
+    [num_pages][heads_kv][page] (e4m3) or [..][4] (e2m1), table int32
     [b][max_pages]."""
     k: object
     v: object
@@ -648,25 +650,33 @@ class DeviceCache:
     def alloc(p: CacheParams, device="cuda") -> "DeviceCache":
         """Pages of undefined contents; every table entry -1 (no page)."""
         import torch
-        eight = p.type == CACHE_E4M3
-        shape = (p.num_pages, p.heads_kv, p.page)
-        pages = lambda: (torch.empty(*shape, p.head_dim, dtype=torch.uint8, device=device).view(torch.float8_e4m3fn)
-                         if eight else torch.empty(*shape, p.head_dim, dtype=torch.bfloat16, device=device))
-        exps = lambda: torch.empty(shape, dtype=torch.uint8, device=device) if eight else None
+        held, pages_shape, exps_shape = DeviceCache._layout(p)
+        eight = held is torch.float8_e4m3fn
+        pages = lambda: (torch.empty(pages_shape, dtype=torch.uint8, device=device).view(held) if eight
+                         else torch.empty(pages_shape, dtype=held, device=device))
+        exps = lambda: torch.empty(exps_shape, dtype=torch.uint8, device=device) if exps_shape else None
         return DeviceCache(pages(), pages(), exps(), exps(),
                            torch.full((p.batch, p.max_pages), -1, dtype=torch.int32, device=device))
+
+    @staticmethod
+    def _layout(p: CacheParams):
+        """(dtype, shape of k and v, shape of the exponents or None)."""
+        import torch
+        shape = (p.num_pages, p.heads_kv, p.page)
+        if p.type == CACHE_E2M1:
+            return torch.uint8, (*shape, p.head_dim // 2), (*shape, p.head_dim // 32)
+        if p.type == CACHE_E4M3:
+            return torch.float8_e4m3fn, (*shape, p.head_dim), shape
+        return torch.bfloat16, (*shape, p.head_dim), None
 
     def checked(self, p: CacheParams, where: str, device: int) -> CacheC:
         """The C struct, once every tensor fits `p` (ValueError otherwise)."""
         import torch
-        shape = (p.num_pages, p.heads_kv, p.page)
-        eight = p.type == CACHE_E4M3
-        held = torch.float8_e4m3fn if eight else torch.bfloat16
-        pages = (*shape, p.head_dim)
+        held, pages, shape = self._layout(p)
         return CacheC(_dense(where, "cache k", self.k, held, pages, device),
                       _dense(where, "cache v", self.v, held, pages, device),
-                      _dense(where, "k_exp", self.k_exp, torch.uint8, shape, device) if eight else None,
-                      _dense(where, "v_exp", self.v_exp, torch.uint8, shape, device) if eight else None,
+                      _dense(where, "k_exp", self.k_exp, torch.uint8, shape, device) if shape else None,
+                      _dense(where, "v_exp", self.v_exp, torch.uint8, shape, device) if shape else None,
                       _dense(where, "table", self.table, torch.int32, (p.batch, p.max_pages), device))
 
 
