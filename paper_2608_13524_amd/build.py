@@ -17,7 +17,7 @@ INCLUDE = os.path.join(ROOT, "include")
 BUILD_DIR = os.path.join(ROOT, "_build")
 LIB_PATH = os.path.join(PKG, "libdartree.so")
 SOURCES = ["api.cpp", "proj.hip", "proj_tile.hip", "lse_topk.hip", "tree.hip", "shared.hip", "heap.hip", "verify.hip", "calib.hip",
-           "serve_api.cpp", "cache.hip", "paged.hip", "sample.hip"]
+           "serve_api.cpp", "cache.hip", "paged.hip", "sample.hip", "pages.hip", "rotary.hip"]
 ARCH = "gfx950"
 
 FLAGS = [

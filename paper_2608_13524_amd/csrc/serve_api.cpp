@@ -1,7 +1,9 @@
-// C ABI of the serving operators (dartree/serve.h): argument checks, then one
-// launcher each.  Nothing here touches the device before every check passed.
+// C ABI of the serving operators (dartree/serve.h, pages.h, rotary.h): argument
+// checks, then one launcher each.  Nothing here touches the device before every check passed.
 #include <math.h>
 
+#include "pages.hpp"
+#include "rotary.hpp"
 #include "serve.hpp"
 
 using namespace dartree;
@@ -85,6 +87,66 @@ dartree_status check_tree(int32_t batch, int32_t budget, int32_t max_len, int32_
 dartree_status check_chain(int32_t batch, int32_t depth, int32_t vocab, int32_t type, float t) {
   if (depth > DARTREE_MAX_DEPTH) return DARTREE_ERR_UNSUPPORTED;
   return check_verify(batch, depth, 2 * depth + 1, vocab, type, t);
+}
+
+dartree_status check_table(const dartree_cache_params* p) {
+  const dartree_status s = check_cache(p);
+  if (s != DARTREE_OK) return s;
+  return int64_t(p->batch) * p->max_pages > (int64_t(1) << 30) ? DARTREE_ERR_UNSUPPORTED : DARTREE_OK;
+}
+
+bool apart(const void* a, int64_t a_bytes, const void* b, int64_t b_bytes) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return x + a_bytes <= y || y + b_bytes <= x;
+}
+
+// A table and what becomes of it: the same memory (where that may be) or none in common.
+bool tables_ok(const dartree_cache_params& p, const int32_t* table, const int32_t* out, bool same) {
+  const int64_t bytes = int64_t(p.batch) * p.max_pages * 4;
+  return given(table) && given(out) && ((same && table == out) || apart(table, bytes, out, bytes));
+}
+
+PagesArgs pages_of(const dartree_cache_params& p, const int32_t* table, int32_t* out) {
+  PagesArgs a{};
+  a.batch = p.batch;
+  while ((1 << a.page_log2) < p.page) ++a.page_log2;
+  a.num_pages = p.num_pages;
+  a.max_pages = p.max_pages;
+  a.table = table;
+  a.out = out;
+  return a;
+}
+
+dartree_status check_rotary(const dartree_rotary_params* p) {
+  if (!p) return DARTREE_ERR_INVALID_ARG;
+  if (p->batch < 1 || p->rows < 1 || p->heads_q < 0 || p->heads_kv < 0 || p->heads_q + int64_t(p->heads_kv) < 1)
+    return DARTREE_ERR_INVALID_ARG;
+  if (p->head_dim < 1 || p->rotary_dim < 2 || p->rotary_dim % 2 != 0 || p->rotary_dim > p->head_dim)
+    return DARTREE_ERR_INVALID_ARG;
+  if (p->layout != DARTREE_ROTARY_HALF && p->layout != DARTREE_ROTARY_INTERLEAVED) return DARTREE_ERR_INVALID_ARG;
+  if (p->type != DARTREE_FP32 && p->type != DARTREE_BF16) return DARTREE_ERR_INVALID_ARG;
+  if (p->inverse != 0 && p->inverse != 1) return DARTREE_ERR_INVALID_ARG;
+  if (!isfinite(p->amplitude)) return DARTREE_ERR_INVALID_ARG;
+  if (p->head_dim % 8 != 0 || p->head_dim > 512 || p->heads_q > 2048 || p->heads_kv > 2048) return DARTREE_ERR_UNSUPPORTED;
+  // a launch holds fewer than 2^32 threads: 256 for a row
+  return double(p->batch) * p->rows > double(1 << 24) - 1 ? DARTREE_ERR_UNSUPPORTED : DARTREE_OK;
+}
+
+// Rows of one of rotary's tensors and of its output.
+bool rotary_rows_ok(const dartree_rotary_params& p, int heads, const void* x, int64_t stride, const void* out,
+                    int64_t out_stride) {
+  if (heads == 0) return true;
+  const int64_t row = int64_t(heads) * p.head_dim;
+  return given(x) && given(out) && stride_ok(stride, row) && stride_ok(out_stride, row) && (x != out || stride == out_stride);
+}
+
+// The fraction of a turn in `radians`, in units of 2^-64 (x87's 64 bits of mantissa).
+uint64_t turn_of(long double radians) {
+  const long double pi = 3.14159265358979323846264338327950288L;
+  long double t = fmodl(radians / (2 * pi), 1.0L);
+  if (t < 0) t += 1.0L;
+  const long double u = floorl(t * 18446744073709551616.0L + 0.5L);
+  return u >= 18446744073709551616.0L ? 0 : uint64_t(u);
 }
 
 }  // namespace
@@ -262,6 +324,159 @@ dartree_status dartree_verify_chain(int32_t batch, int32_t depth, int32_t vocab,
   a.bonus = bonus;
   a.ws = ws;
   return hip_status(launch_verify_chain(a, stream));
+}
+
+dartree_status dartree_pages_workspace_size(const dartree_cache_params* p, size_t* bytes) {
+  if (!bytes) return DARTREE_ERR_INVALID_ARG;
+  const dartree_status s = check_table(p);
+  if (s != DARTREE_OK) return s;
+  *bytes = pages_workspace(p->batch, p->num_pages);
+  return DARTREE_OK;
+}
+
+dartree_status dartree_pages_fork(const dartree_cache_params* p, const int32_t* table, int32_t* out,
+                                  const int32_t* source, const int32_t* keep, hipStream_t stream) {
+  const dartree_status s = check_table(p);
+  if (s != DARTREE_OK) return s;
+  if (!tables_ok(*p, table, out, !source) || !optional(source) || !optional(keep)) return DARTREE_ERR_INVALID_ARG;
+  PagesArgs a = pages_of(*p, table, out);
+  a.source = source;
+  a.keep = keep;
+  return hip_status(launch_pages_fork(a, stream));
+}
+
+dartree_status dartree_pages_reserve(const dartree_cache_params* p, const int32_t* table, int32_t* out, int32_t rows,
+                                     const int32_t* start, const int32_t* counts, int32_t* pairs, int32_t max_pairs,
+                                     int32_t* totals, int32_t* granted, void* ws, size_t ws_bytes, hipStream_t stream) {
+  const dartree_status s = check_table(p);
+  if (s != DARTREE_OK) return s;
+  if (rows < 1) return DARTREE_ERR_INVALID_ARG;
+  if (!tables_ok(*p, table, out, true) || !optional(start) || !optional(counts) || !given(pairs) || !given(totals) ||
+      !given(granted))
+    return DARTREE_ERR_INVALID_ARG;
+  const int64_t columns = (int64_t(rows) + p->page - 2) / p->page + 1;
+  PagesArgs a = pages_of(*p, table, out);
+  a.columns = int(columns < p->max_pages ? columns : p->max_pages);
+  if (max_pairs < int64_t(p->batch) * a.columns) return DARTREE_ERR_INVALID_ARG;
+  if (!workspace_fits(ws, ws_bytes, pages_workspace(p->batch, p->num_pages))) return DARTREE_ERR_WORKSPACE;
+  a.rows = rows;
+  a.start = start;
+  a.counts = counts;
+  a.pairs = pairs;
+  a.totals = totals;
+  a.granted = granted;
+  a.ws = ws;
+  return hip_status(launch_pages_reserve(a, stream));
+}
+
+dartree_status dartree_pages_compact(const dartree_cache_params* p, const int32_t* table, int32_t* out, int32_t* pairs,
+                                     int32_t max_pairs, int32_t* totals, void* ws, size_t ws_bytes, hipStream_t stream) {
+  const dartree_status s = check_table(p);
+  if (s != DARTREE_OK) return s;
+  if (!tables_ok(*p, table, out, true) || !optional(pairs) || (!pairs && p->num_pages > 1) || !given(totals) ||
+      max_pairs < p->num_pages / 2)
+    return DARTREE_ERR_INVALID_ARG;
+  if (!workspace_fits(ws, ws_bytes, pages_workspace(p->batch, p->num_pages))) return DARTREE_ERR_WORKSPACE;
+  PagesArgs a = pages_of(*p, table, out);
+  a.pairs = pairs;
+  a.totals = totals;
+  a.ws = ws;
+  return hip_status(launch_pages_compact(a, stream));
+}
+
+dartree_status dartree_cache_copy(const dartree_cache_params* p, const dartree_cache* cache, const int32_t* pairs,
+                                  int32_t max_pairs, const int32_t* count, hipStream_t stream) {
+  const dartree_status s = check_cache(p);
+  if (s != DARTREE_OK) return s;
+  if (!cache || !given(cache->k) || !given(cache->v) || !given(pairs) || !given(count) || max_pairs < 1)
+    return DARTREE_ERR_INVALID_ARG;
+  const int bits = bits_of(*p);
+  if (bits != 16 && (!given(cache->k_exp) || !given(cache->v_exp))) return DARTREE_ERR_INVALID_ARG;
+  const int64_t rows = int64_t(p->heads_kv) * p->page;
+  PageCopyArgs a{};
+  a.num_pages = p->num_pages;
+  a.row_bytes = rows * kHead * bits / 8;
+  a.exp_bytes = bits == 16 ? 0 : bits == 8 ? rows : rows * (kHead / kBlock);
+  a.k = cache->k;
+  a.v = cache->v;
+  a.k_exp = cache->k_exp;
+  a.v_exp = cache->v_exp;
+  a.pairs = pairs;
+  a.max_pairs = max_pairs;
+  a.count = count;
+  return hip_status(launch_cache_copy(a, stream));
+}
+
+dartree_status dartree_rotary_turns(int32_t rotary_dim, double base, const dartree_rotary_scaling* scaling,
+                                    uint64_t* turns) {
+  if (!turns || rotary_dim < 2 || rotary_dim % 2 != 0 || !isfinite(base) || !(base > 0)) return DARTREE_ERR_INVALID_ARG;
+  if (rotary_dim > 512) return DARTREE_ERR_UNSUPPORTED;
+  const int rule = scaling ? scaling->rule : DARTREE_ROTARY_PLAIN;
+  if (rule < DARTREE_ROTARY_PLAIN || rule > DARTREE_ROTARY_TURNS) return DARTREE_ERR_INVALID_ARG;
+  const long double factor = rule == DARTREE_ROTARY_PLAIN ? 1.0L : (long double)scaling->factor;
+  if (rule != DARTREE_ROTARY_PLAIN && (!isfinite(scaling->factor) || !(scaling->factor > 0))) return DARTREE_ERR_INVALID_ARG;
+  if (rule == DARTREE_ROTARY_TURNS && (!isfinite(scaling->low) || !isfinite(scaling->high) || !(scaling->low < scaling->high) ||
+                                       scaling->length < 1))
+    return DARTREE_ERR_INVALID_ARG;
+  const long double r = rotary_dim, pi = 3.14159265358979323846264338327950288L;
+  long double b = base;
+  if (rule == DARTREE_ROTARY_BASE && rotary_dim > 2) b *= powl(factor, r / (r - 2));
+  for (int i = 0; i < rotary_dim / 2; ++i) {
+    long double f = powl(b, -2 * i / r);
+    if (rule == DARTREE_ROTARY_LINEAR) f /= factor;
+    if (rule == DARTREE_ROTARY_TURNS) {
+      long double s = (scaling->length * f / (2 * pi) - scaling->low) / ((long double)scaling->high - scaling->low);
+      s = s < 0 ? 0 : s > 1 ? 1 : s;
+      f *= s + (1 - s) / factor;
+    }
+    turns[i] = turn_of(f);
+  }
+  return DARTREE_OK;
+}
+
+dartree_status dartree_rotary_turns_of(int32_t pairs, const double* radians, uint64_t* turns) {
+  if (pairs < 1 || !radians || !turns) return DARTREE_ERR_INVALID_ARG;
+  for (int i = 0; i < pairs; ++i)
+    if (!isfinite(radians[i])) return DARTREE_ERR_INVALID_ARG;
+  for (int i = 0; i < pairs; ++i) turns[i] = turn_of(radians[i]);
+  return DARTREE_OK;
+}
+
+dartree_status dartree_rotary(const dartree_rotary_params* p, const uint64_t* turns, const void* q, int64_t q_stride,
+                              const void* k, int64_t k_stride, void* q_out, int64_t q_out_stride, void* k_out,
+                              int64_t k_out_stride, const int32_t* positions, const int32_t* start,
+                              const int32_t* counts, hipStream_t stream) {
+  const dartree_status s = check_rotary(p);
+  if (s != DARTREE_OK) return s;
+  if (!given(turns) || !optional(positions) || !optional(start) || !optional(counts)) return DARTREE_ERR_INVALID_ARG;
+  if (!rotary_rows_ok(*p, p->heads_q, q, q_stride, q_out, q_out_stride) ||
+      !rotary_rows_ok(*p, p->heads_kv, k, k_stride, k_out, k_out_stride))
+    return DARTREE_ERR_INVALID_ARG;
+  RotaryArgs a{};
+  a.batch = p->batch;
+  a.rows = p->rows;
+  a.heads_q = p->heads_q;
+  a.heads_kv = p->heads_kv;
+  a.head_dim = p->head_dim;
+  a.rotary_dim = p->rotary_dim;
+  a.layout = p->layout;
+  a.bf16 = p->type == DARTREE_BF16;
+  a.inverse = p->inverse;
+  a.first = p->first;
+  a.amplitude = p->amplitude;
+  a.turns = turns;
+  a.q = q;
+  a.k = k;
+  a.q_out = q_out;
+  a.k_out = k_out;
+  a.q_stride = q_stride;
+  a.k_stride = k_stride;
+  a.q_out_stride = q_out_stride;
+  a.k_out_stride = k_out_stride;
+  a.positions = positions;
+  a.start = start;
+  a.counts = counts;
+  return hip_status(launch_rotary(a, stream));
 }
 
 }  // extern "C"

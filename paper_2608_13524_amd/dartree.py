@@ -21,6 +21,9 @@ HEAD_MARKOV = 1
 CACHE_BF16 = 0
 CACHE_E4M3 = 1
 CACHE_E2M1 = 4
+ROTARY_HALF = 0
+ROTARY_INTERLEAVED = 1
+ROTARY_PLAIN, ROTARY_LINEAR, ROTARY_BASE, ROTARY_TURNS = range(4)
 
 OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_WORKSPACE, ERR_HIP, ERR_ORDER, ERR_NONFINITE = range(7)
 
@@ -55,6 +58,13 @@ SERVE_SYMBOLS = [
     "dartree_verify_tree_workspace_size", "dartree_verify_tree",
     "dartree_verify_chain_workspace_size", "dartree_verify_chain",
 ]
+# include/dartree/pages.h
+PAGES_SYMBOLS = [
+    "dartree_pages_workspace_size", "dartree_pages_fork", "dartree_pages_reserve", "dartree_pages_compact",
+    "dartree_cache_copy",
+]
+# include/dartree/rotary.h
+ROTARY_SYMBOLS = ["dartree_rotary_turns", "dartree_rotary_turns_of", "dartree_rotary"]
 CALIB_MAX_BARRIERS = 64
 CALIB_SINK_FLOATS = 4096
 
@@ -119,6 +129,19 @@ class CacheParams(ctypes.Structure):
 class CacheC(ctypes.Structure):
     _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_exp", ctypes.c_void_p),
                 ("v_exp", ctypes.c_void_p), ("table", ctypes.c_void_p)]
+
+
+class RotaryScaling(ctypes.Structure):
+    """A rule for contexts longer than the trained ones (include/dartree/rotary.h)."""
+    _fields_ = [("rule", ctypes.c_int32), ("factor", ctypes.c_double), ("low", ctypes.c_double), ("high", ctypes.c_double),
+                ("length", ctypes.c_int32)]
+
+
+class RotaryParams(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("rows", ctypes.c_int32), ("heads_q", ctypes.c_int32),
+                ("heads_kv", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("rotary_dim", ctypes.c_int32),
+                ("layout", ctypes.c_int32), ("type", ctypes.c_int32), ("inverse", ctypes.c_int32),
+                ("first", ctypes.c_int32), ("amplitude", ctypes.c_float)]
 
 
 class DartreeError(RuntimeError):
@@ -187,7 +210,15 @@ def lib() -> ctypes.CDLL:
     L.dartree_verify_tree.argtypes = [i32, i32, i32, i32, i32, vp, vp, vp, vp, i64, f32, vp, vp, vp, vp, vp, sz, vp]
     L.dartree_verify_chain_workspace_size.argtypes = [i32, i32, i32, ctypes.POINTER(sz)]
     L.dartree_verify_chain.argtypes = [i32, i32, i32, i32, vp, vp, vp, vp, i64, f32, vp, vp, vp, vp, sz, vp]
-    for name in SYMBOLS + SERVE_SYMBOLS:
+    L.dartree_pages_workspace_size.argtypes = [C, ctypes.POINTER(sz)]
+    L.dartree_pages_fork.argtypes = [C, vp, vp, vp, vp, vp]
+    L.dartree_pages_reserve.argtypes = [C, vp, vp, i32, vp, vp, vp, i32, vp, vp, vp, sz, vp]
+    L.dartree_pages_compact.argtypes = [C, vp, vp, vp, i32, vp, vp, sz, vp]
+    L.dartree_cache_copy.argtypes = [C, ctypes.POINTER(CacheC), vp, i32, vp, vp]
+    L.dartree_rotary_turns.argtypes = [i32, ctypes.c_double, ctypes.POINTER(RotaryScaling), vp]
+    L.dartree_rotary_turns_of.argtypes = [i32, vp, vp]
+    L.dartree_rotary.argtypes = [ctypes.POINTER(RotaryParams), vp, vp, i64, vp, i64, vp, i64, vp, i64, vp, vp, vp, vp]
+    for name in SYMBOLS + SERVE_SYMBOLS + PAGES_SYMBOLS + ROTARY_SYMBOLS:
         if name not in ("dartree_abi_version", "dartree_status_string"):
             getattr(L, name).restype = ctypes.c_int
     _lib = L
@@ -822,3 +853,133 @@ def verify_chain(tokens, target_logits, draft_logits, temperature: float, unifor
     _on_device(where, device)
     _check(lib().dartree_verify_chain(b, n, vocab, FP32 if target_logits.dtype is torch.float32 else BF16, tp, np_, zp, dp,
                                       step, temperature, up, cp, bp, wp, nbytes, st), "dartree_verify_chain")
+
+
+# ---------------------------------------------------------------------------
+# Serving: the pages of a cache (dartree/pages.h)
+# ---------------------------------------------------------------------------
+def pages_workspace_size(p: CacheParams) -> int:
+    n = ctypes.c_size_t(0)
+    _check(lib().dartree_pages_workspace_size(ctypes.byref(p), ctypes.byref(n)), "dartree_pages_workspace_size")
+    return n.value
+
+
+def pages_fork(p: CacheParams, table, out, source=None, keep=None, stream=None) -> None:
+    """Row q of out int32 [b][max_pages]: the entries of row source[q] (None: q) of
+    table that hold its first keep[q] positions (None: all), -1 behind them."""
+    import torch
+    where, i32 = "pages_fork", torch.int32
+    device, st = _place(stream)
+    shape = (p.batch, p.max_pages)
+    tp = _dense(where, "table", table, i32, shape, device)
+    op = _dense(where, "out", out, i32, shape, device)
+    sp = _dense(where, "source", source, i32, (p.batch,), device)
+    kp = _dense(where, "keep", keep, i32, (p.batch,), device)
+    _on_device(where, device)
+    _check(lib().dartree_pages_fork(ctypes.byref(p), tp, op, sp, kp, st), "dartree_pages_fork")
+
+
+def _pairs(where: str, pairs, device: int):
+    """(address, rows) of a list of pages [max_pairs][2]."""
+    import torch
+    n = pairs.shape[0] if pairs.dim() == 2 else -1
+    return _dense(where, "pairs", pairs, torch.int32, (n, 2), device), n
+
+
+def pages_reserve(p: CacheParams, table, out, rows: int, start, counts, pairs, totals, granted, ws, stream=None) -> None:
+    """Pages for positions start[q] (None: 0) .. start[q] + counts[q] - 1 (None: rows,
+    the most of a request): out is table with free pages in the place of absent and
+    shared ones; pairs int32 [max_pairs][2] of the shared, totals int32 [2] = {pairs
+    listed, free pages left}, granted int32 [b]."""
+    import torch
+    where, i32 = "pages_reserve", torch.int32
+    device, st = _place(stream)
+    shape, b = (p.batch, p.max_pages), (p.batch,)
+    tp = _dense(where, "table", table, i32, shape, device)
+    op = _dense(where, "out", out, i32, shape, device)
+    sp = _dense(where, "start", start, i32, b, device)
+    cp = _dense(where, "counts", counts, i32, b, device)
+    pp, n = _pairs(where, pairs, device)
+    np_ = _dense(where, "totals", totals, i32, (2,), device)
+    gp = _dense(where, "granted", granted, i32, b, device)
+    wp, nbytes = _workspace(where, ws, device)
+    _on_device(where, device)
+    _check(lib().dartree_pages_reserve(ctypes.byref(p), tp, op, rows, sp, cp, pp, n, np_, gp, wp, nbytes, st),
+           "dartree_pages_reserve")
+
+
+def pages_compact(p: CacheParams, table, out, pairs, totals, ws, stream=None) -> None:
+    """out: table with the pages in use moved to the front of the pool; pairs int32
+    [max_pairs >= num_pages / 2][2], totals int32 [2] = {pairs listed, pages in use}."""
+    import torch
+    where, i32 = "pages_compact", torch.int32
+    device, st = _place(stream)
+    shape = (p.batch, p.max_pages)
+    tp = _dense(where, "table", table, i32, shape, device)
+    op = _dense(where, "out", out, i32, shape, device)
+    pp, n = _pairs(where, pairs, device)
+    np_ = _dense(where, "totals", totals, i32, (2,), device)
+    wp, nbytes = _workspace(where, ws, device)
+    _on_device(where, device)
+    _check(lib().dartree_pages_compact(ctypes.byref(p), tp, op, pp, n, np_, wp, nbytes, st), "dartree_pages_compact")
+
+
+def cache_copy(p: CacheParams, cache: DeviceCache, pairs, count, stream=None) -> None:
+    """Pages pairs[i][0] of the cache to pairs[i][1], i < count[0] (int32 on the
+    device: the totals of pages_reserve or pages_compact)."""
+    import torch
+    where = "cache_copy"
+    device, st = _place(stream)
+    cc = cache.checked(p, where, device)
+    pp, n = _pairs(where, pairs, device)
+    np_ = _dense(where, "count", count, torch.int32, tuple(count.shape), device)
+    if count.numel() < 1:
+        raise ValueError(f"{where}: count is empty")
+    _on_device(where, device)
+    _check(lib().dartree_cache_copy(ctypes.byref(p), ctypes.byref(cc), pp, n, np_, st), "dartree_cache_copy")
+
+
+# ---------------------------------------------------------------------------
+# Rotary positions (dartree/rotary.h)
+# ---------------------------------------------------------------------------
+def rotary_turns(rotary_dim: int, base: float = 10000.0, scaling: Optional[RotaryScaling] = None, device="cuda"):
+    """The table of frequencies that `rotary` reads, int64 [rotary_dim / 2]."""
+    host = (ctypes.c_uint64 * max(rotary_dim // 2, 1))()
+    _check(lib().dartree_rotary_turns(rotary_dim, base, None if scaling is None else ctypes.byref(scaling), host),
+           "dartree_rotary_turns")
+    return _turns(host, device)
+
+
+def rotary_turns_of(radians, device="cuda"):
+    """The same table of any frequencies, in radians a position."""
+    f = (ctypes.c_double * max(len(radians), 1))(*radians)
+    host = (ctypes.c_uint64 * max(len(radians), 1))()
+    _check(lib().dartree_rotary_turns_of(len(radians), f, host), "dartree_rotary_turns_of")
+    return _turns(host, device)
+
+
+def _turns(host, device):
+    import torch
+    return torch.tensor([x - (1 << 64) if x >> 63 else x for x in host], dtype=torch.int64, device=device)
+
+
+def rotary(p: RotaryParams, turns, q, k, q_out, k_out, positions=None, start=None, counts=None, stream=None) -> None:
+    """q [b][rows][heads_q][head_dim] and k [b][rows][heads_kv][head_dim] (None
+    without heads; rows of a wider tensor are taken as they are) turned by their
+    rows' positions first + start[r] + positions[r][i] (None: 0, i) into q_out and
+    k_out, which may be q and k; all bfloat16 or all float32 (p.type).  Rows at and
+    past counts[r] are left as they were."""
+    import torch
+    where, i32 = "rotary", torch.int32
+    device, st = _place(stream)
+    b, rows = p.batch, p.rows
+    dtypes = (torch.bfloat16,) if p.type == BF16 else (torch.float32,)
+    args = []
+    for name, x, heads in (("q", q, p.heads_q), ("k", k, p.heads_kv), ("q_out", q_out, p.heads_q), ("k_out", k_out, p.heads_kv)):
+        args += [None, 0] if heads == 0 else _rows(where, name, x, dtypes, (b, rows, heads, p.head_dim), device)
+    tp = _dense(where, "turns", turns, torch.int64, (p.rotary_dim // 2,), device)
+    pp = _dense(where, "positions", positions, i32, (b, rows), device)
+    sp = _dense(where, "start", start, i32, (b,), device)
+    cp = _dense(where, "counts", counts, i32, (b,), device)
+    _on_device(where, device)
+    _check(lib().dartree_rotary(ctypes.byref(p), tp, *args, pp, sp, cp, st), "dartree_rotary")
