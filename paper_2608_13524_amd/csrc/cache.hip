@@ -26,13 +26,6 @@ __device__ __forceinline__ int64_t slot_of(const CacheView& c, int q, int64_t po
   return ((int64_t(page) * c.heads_kv) << c.page_log2) + (pos & ((1 << c.page_log2) - 1));
 }
 
-// Least e >= kExpLow with amax <= 448 * 2^e = 1.75 * 2^(e + 8).
-__device__ __forceinline__ int row_exponent(float amax) {
-  const uint32_t u = __float_as_uint(amax);
-  const int e = int(u >> 23) - 127 - 8 + ((u & 0x7FFFFFu) > 0x600000u);
-  return min(max(e, kExpLow), 120);
-}
-
 __device__ __forceinline__ float low(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float high(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
 

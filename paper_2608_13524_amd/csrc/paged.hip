@@ -32,6 +32,7 @@ namespace dartree {
 namespace {
 
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef int i32x8 __attribute__((ext_vector_type(8)));
 
 constexpr int kChunk = 32;            // keys of a wave's share of a step
 
@@ -65,6 +66,66 @@ __device__ __forceinline__ uint32_t without_odd(uint32_t w) {
 }
 __device__ __forceinline__ float odd_part(uint16_t v) {
   return (v & 0x7F80u) == 0x7F80u ? __uint_as_float(uint32_t(v) << 16) : 0.f;
+}
+
+// A query's row for products with keys in e2m1, which the matrix instruction takes as
+// they are, 128 dims at once, with the exponent byte of each 32.  Its other operand is
+// 8 bits wide, so a query goes in two parts, e4m3 of q 2^-e and e4m3 of 2^4 times what
+// that leaves: 4 + 4 bits hold the 8 of a bf16 number, down to 2^-13 under a largest of
+// 224 .. 448 (e is that of its 32 dims), so an element is off by 2^-14 / 224 = 2^-21.8 of
+// the largest of its 32 at most.  The two products take the matrix cores as long as four
+// of bf16 do (34 cycles each), without converting the keys and with a quarter of
+// their bytes.  An infinity or a NaN makes a NaN of its row's scores.
+struct Parts4 {
+  i32x8 hi, lo;
+  int scale;      // bytes: exponents of the 32 dims that are this lane's in the instruction's order, of hi and of lo
+};
+__device__ __forceinline__ Parts4 query_parts(const uint16_t* q) {
+  typedef float f32x2 __attribute__((ext_vector_type(2)));
+  const int lane = threadIdx.x & 63, g = lane >> 4;
+  Parts4 r;
+  int e[2];   // a lane has dims 16 g .. + 15 and 64 + 16 g .. + 15
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    float f[16], m = 0.f;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const u32x4 x = *reinterpret_cast<const u32x4*>(q + 64 * h + 16 * g + 8 * i);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        f[8 * i + 2 * j] = __uint_as_float(x[j] << 16);
+        f[8 * i + 2 * j + 1] = __uint_as_float(x[j] & 0xFFFF0000u);
+        m = fmaxf(m, fmaxf(fabsf(f[8 * i + 2 * j]), fabsf(f[8 * i + 2 * j + 1])));
+      }
+    }
+    m = fmaxf(m, __shfl_xor(m, 16));
+    e[h] = row_exponent<-122>(m);   // as low as the exponent byte of lo goes: the least normal numbers keep their bits
+    const float s = __uint_as_float(uint32_t(127 - e[h]) << 23);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float a = f[4 * i] * s, b = f[4 * i + 1] * s, c = f[4 * i + 2] * s, d = f[4 * i + 3] * s;
+      int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+      w = __builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
+      const f32x2 ab = __builtin_amdgcn_cvt_pk_f32_fp8(w, false), cd = __builtin_amdgcn_cvt_pk_f32_fp8(w, true);
+      int v = __builtin_amdgcn_cvt_pk_fp8_f32((a - ab[0]) * 16.f, (b - ab[1]) * 16.f, 0, false);
+      v = __builtin_amdgcn_cvt_pk_fp8_f32((c - cd[0]) * 16.f, (d - cd[1]) * 16.f, v, true);
+      r.hi[4 * h + i] = w;
+      r.lo[4 * h + i] = v;
+    }
+  }
+  const int of = (lane & 15) + 32 * (g & 1);   // dims 32 g .. + 31 are halves g / 2 of lane groups 2 (g % 2) and the next
+  const int e0 = __shfl(e[0], of), e1 = __shfl(e[1], of);
+  const int own = (g < 2 ? e0 : e1) + 127;
+  r.scale = own | ((own - 4) << 8);
+  return r;
+}
+// Scores of 16 keys; byte T of `scale`: the exponent of the key's 32 dims.
+template <int T>
+__device__ __forceinline__ f32x4 scores4(u32x4 k, int scale, const Parts4& q) {
+  const i32x8 a{int(k[0]), int(k[1]), int(k[2]), int(k[3]), 0, 0, 0, 0};
+  f32x4 s{0.f, 0.f, 0.f, 0.f};
+  s = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, q.hi, s, 4, 0, T, scale, 0, q.scale);
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, q.lo, s, 4, 0, T, scale, 1, q.scale);
 }
 
 template <bool HI>
@@ -203,9 +264,7 @@ __device__ __forceinline__ void chunk_scores(const Chunk<BITS>& c, const u32x4 (
 #pragma unroll
     for (int ks = 0; ks < 4; ++ks) {
       u32x4 kf;
-      if constexpr (BITS == 4) {
-        kf = expand8(c.k[t][0][ks], __uint_as_float(c.ke[t] << 23));
-      } else if constexpr (BITS == 8) {
+      if constexpr (BITS == 8) {
         const float sc = __uint_as_float(uint32_t(c.ke[t]) << 23);
         const uint32_t w0 = c.k[t][ks >> 1][2 * (ks & 1)], w1 = c.k[t][ks >> 1][2 * (ks & 1) + 1];
         kf = u32x4{expand2<false>(w0, sc), expand2<true>(w0, sc), expand2<false>(w1, sc), expand2<true>(w1, sc)};
@@ -345,10 +404,14 @@ __global__ __launch_bounds__(64 * W, 8 / W) void paged_attention(PagedArgs a, in
     const int row = min(rt * 16 + c16, rows - 1);   // past the end: the last row, never stored
     const int node = row / a.group;
     const int64_t from = (int64_t(q) * a.budget + node) * a.q_stride + (kvh * a.group + row - node * a.group) * kHead;
-    // operand ks: eight dims from here on, for keys alike (e2m1: a lane's dims are one block)
-    auto dim_of = [&](int ks) { return BITS == 4 ? 32 * g + 8 * ks : 64 * (ks >> 1) + 16 * g + 8 * (ks & 1); };
+    Parts4 qp;
+    // operand ks: dims 64 (ks / 2) + 16 g + 8 (ks % 2) .. + 7, for keys alike
+    auto load_query = [&] {
 #pragma unroll
-    for (int ks = 0; ks < 4; ++ks) qf[ks] = *reinterpret_cast<const u32x4*>(a.q + from + dim_of(ks));
+      for (int ks = 0; ks < 4; ++ks)
+        qf[ks] = *reinterpret_cast<const u32x4*>(a.q + from + 64 * (ks >> 1) + 16 * g + 8 * (ks & 1));
+    };
+    if constexpr (BITS != 4) load_query();
     const uint32_t* mrow = a.mask ? reinterpret_cast<const uint32_t*>(a.mask) + (int64_t(q) * a.budget + node) * words : nullptr;
     clear(st);
 
@@ -360,6 +423,7 @@ __global__ __launch_bounds__(64 * W, 8 / W) void paged_attention(PagedArgs a, in
     const int chunks = kb0 < ex.ctx ? min(min(step + n, nctx) - step, (ex.ctx - kb0 + kStep - 1) / kStep) : 0;
     if (chunks > 0) {
       Chunk<BITS> ch;
+      if constexpr (BITS == 4) qp = query_parts(a.q + from);
       f32x4 sc[2];
       u32x4 p;
       int p0, p1;   // pages of the halves of the chunk to fetch next
@@ -426,7 +490,12 @@ __global__ __launch_bounds__(64 * W, 8 / W) void paged_attention(PagedArgs a, in
           const int kb = kb0 + (i + 1) * kStep;
           const bool more = i + 1 < chunks;
           if (more) look_up(kb);
-          chunk_scores<BITS, TOP.value>(ch, qf, sc);
+          if constexpr (BITS == 4) {
+#pragma unroll
+            for (int t = 0; t < 2; ++t) sc[t] = scores4<0>(ch.k[t][0], int(ch.ke[t]), qp);
+          } else {
+            chunk_scores<BITS, TOP.value>(ch, qf, sc);
+          }
           uint32_t e0 = BITS == 8 ? ch.ke[0] : 0, e1 = BITS == 8 ? ch.ke[1] : 0;
           if (more) fetch_keys(kb);
           if constexpr (BITS == 8 && !TOP.value) {
@@ -463,6 +532,7 @@ __global__ __launch_bounds__(64 * W, 8 / W) void paged_attention(PagedArgs a, in
       return mrow ? mrow[kb >> 5] : node < kb ? 0u : node - kb >= 31 ? ~0u : (2u << (node - kb)) - 1u;
     };
     bool odd = false;   // the same for the wave
+    if constexpr (BITS == 4) load_query();
     for (int s = max(step, nctx); s < step + n; ++s) {
       const int kb = (s - nctx) * kStep + wave * kChunk;
       if (kb >= ex.nodes) break;
@@ -474,9 +544,10 @@ __global__ __launch_bounds__(64 * W, 8 / W) void paged_attention(PagedArgs a, in
       Chunk<16> ch;
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
-        const uint16_t* kp = a.k_tree + at(16 * t + c16);
+        const uint16_t* kp = a.k_tree + at(16 * t + c16) + 16 * g;
 #pragma unroll
-        for (int ks = 0; ks < 4; ++ks) ch.k[t][ks] = *reinterpret_cast<const u32x4*>(kp + dim_of(ks));
+        for (int ks = 0; ks < 4; ++ks)
+          ch.k[t][ks] = *reinterpret_cast<const u32x4*>(kp + 64 * (ks >> 1) + 8 * (ks & 1));
       }
 #pragma unroll
       for (int e = 0; e < 8; ++e)
@@ -634,6 +705,18 @@ __global__ __launch_bounds__(64 * W, 8 / W) void paged_tiles(PagedArgs a, int wh
     const int kvh = item / ntile, rt = item - kvh * ntile;
 
     u32x4 qf[RG][4];
+    Parts4 qp[BITS == 4 ? RG : 1];
+    auto load_query = [&] {
+      const int tid = thread_again();
+#pragma unroll
+      for (int r = 0; r < RG; ++r) {
+        const int row = min(rt * kRows + (tid >> 6) * (16 * RG) + r * 16 + (tid & 15), rows - 1);   // past the end: the last row, never stored
+        const int node = row / a.group;
+        const uint16_t* from = a.q + (int64_t(q) * a.budget + node) * a.q_stride + (kvh * a.group + row - node * a.group) * kHead;
+#pragma unroll
+        for (int ks = 0; ks < 4; ++ks) qf[r][ks] = *reinterpret_cast<const u32x4*>(from + 32 * ks + 8 * ((tid & 63) >> 4));
+      }
+    };
     float m[RG], l[RG], bar[RG], ref[RG];   // bar: a score above it moves the reference m; ref = -m c2
     f32x4 o[RG][8];
     {
@@ -642,9 +725,13 @@ __global__ __launch_bounds__(64 * W, 8 / W) void paged_tiles(PagedArgs a, int wh
       for (int r = 0; r < RG; ++r) {
         const int row = min(rt * kRows + (tid >> 6) * (16 * RG) + r * 16 + (tid & 15), rows - 1);   // past the end: the last row, never stored
         const int node = row / a.group;
-        const uint16_t* qp = a.q + (int64_t(q) * a.budget + node) * a.q_stride + (kvh * a.group + row - node * a.group) * kHead;
+        const uint16_t* from = a.q + (int64_t(q) * a.budget + node) * a.q_stride + (kvh * a.group + row - node * a.group) * kHead;
+        if constexpr (BITS == 4) {
+          qp[r] = query_parts(from);
+        } else {
 #pragma unroll
-        for (int ks = 0; ks < 4; ++ks) qf[r][ks] = *reinterpret_cast<const u32x4*>(qp + 32 * ks + 8 * ((tid & 63) >> 4));
+          for (int ks = 0; ks < 4; ++ks) qf[r][ks] = *reinterpret_cast<const u32x4*>(from + 32 * ks + 8 * ((tid & 63) >> 4));
+        }
         m[r] = bar[r] = -INFINITY;
         l[r] = ref[r] = 0.f;
 #pragma unroll
@@ -674,6 +761,21 @@ __global__ __launch_bounds__(64 * W, 8 / W) void paged_tiles(PagedArgs a, int wh
 #pragma unroll
           for (int r = 0; r < RG; ++r) sc[r][t] = mfma16(kf, qf[r][ks], sc[r][t]);
         }
+      }
+    };
+    // the same of keys in e2m1: a row of 64 bytes keeps its 16-byte piece c at c ^ (row / 4) % 4,
+    // behind the rows a word for each lane (r16, g): the exponents of keys r16, 16 + r16, ..
+    auto scores_of_4 = [&](auto B, auto C, f32x4 (&sc)[RG][2]) __attribute__((always_inline)) {
+      LDS_AS char* const kt = lds + B.value * 2 * kTileBytes;
+      const int e = *reinterpret_cast<const LDS_AS int*>(kt + kTile * (kHead / 2) + (4 * r16 + g) * 4);
+      u32x4 kf[2];
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+        kf[t] = *reinterpret_cast<const LDS_AS u32x4*>(kt + (C.value * 32 + t * 16 + r16) * (kHead / 2) + (g ^ (r16 >> 2)) * 16);
+#pragma unroll
+      for (int r = 0; r < RG; ++r) {
+        sc[r][0] = scores4<2 * C.value>(kf[0], e, qp[r]);
+        sc[r][1] = scores4<2 * C.value + 1>(kf[1], e, qp[r]);
       }
     };
     // unseen keys out; the reference of a row moves as in chunk_weights, one test for all rows
@@ -742,7 +844,7 @@ __global__ __launch_bounds__(64 * W, 8 / W) void paged_tiles(PagedArgs a, int wh
     // into registers; store(B): the fetched tile to buffer B, returning which of
     // its keys are there (one that is not has zeros for values: 0 * NaN is NaN);
     // sees(s, r, there): what row group r sees of the keys that are.
-    auto sweep = [&](const int first, const int end, auto&& fetch, auto&& store, auto&& sees, const bool tree) __attribute__((always_inline)) {
+    auto sweep = [&](const int first, const int end, auto&& fetch, auto&& store, auto&& sees, auto&& scores, const bool tree) __attribute__((always_inline)) {
       if (first >= end) return;
       fetch(first);
       uint64_t there = store(Index<0>());
@@ -834,13 +936,15 @@ __global__ __launch_bounds__(64 * W, 8 / W) void paged_tiles(PagedArgs a, int wh
           const bool gone = there != ~0ull && !((there >> key) & 1);
           if (gone) vx[i] = zero;
           if constexpr (BITS == 4) {
-            const float sk = __uint_as_float(ke[i] << 23), sv = gone ? 1.f : __uint_as_float(ve[i] << 23);
+            const float sv = gone ? 1.f : __uint_as_float(ve[i] << 23);
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
               const int c = 2 * (lane & 7) + h;
-              *reinterpret_cast<LDS_AS u32x4*>(kt + key * kRowBytes + (c ^ k_place(key)) * 16) = expand8(kx[i][h], sk);
               *reinterpret_cast<LDS_AS u32x4*>(kt + kTileBytes + key * kRowBytes + (c ^ v_place(key)) * 16) = expand8(vx[i][h], sv);
             }
+            const int c = (lane & 7) >> 1;   // keys stay as they are
+            *reinterpret_cast<LDS_AS u32x2*>(kt + key * (kHead / 2) + (c ^ ((key >> 2) & 3)) * 16 + (lane & 1) * 8) = kx[i];
+            *reinterpret_cast<LDS_AS uint8_t*>(kt + kTile * (kHead / 2) + (4 * (key & 15) + c) * 4 + (key >> 4)) = uint8_t(ke[i]);
           } else if constexpr (BITS == 8) {
             const float sk = __uint_as_float(ke[i] << 23), sv = gone ? 1.f : __uint_as_float(ve[i] << 23);
             u32x4 k[2], v[2];
@@ -872,8 +976,11 @@ __global__ __launch_bounds__(64 * W, 8 / W) void paged_tiles(PagedArgs a, int wh
         return there;
       };
       if (step < min(last, nctx)) look_up(step);
-      sweep(step, min(last, nctx), fetch, store, [&](int, int, uint64_t there) { return there; }, false);
+      auto all = [&](int, int, uint64_t there) { return there; };
+      if constexpr (BITS == 4) sweep(step, min(last, nctx), fetch, store, all, scores_of_4, false);
+      else sweep(step, min(last, nctx), fetch, store, all, scores, false);
     }
+    if constexpr (BITS == 4) load_query();
     const int tid = thread_again();
     int node[RG], row[RG];
 #pragma unroll
@@ -927,7 +1034,7 @@ __global__ __launch_bounds__(64 * W, 8 / W) void paged_tiles(PagedArgs a, int wh
         const int d = node[r] - (s - nctx) * kTile;   // a chain's node sees keys up to its own
         return there & (d < 0 ? 0ull : d >= 63 ? ~0ull : (2ull << d) - 1);
       };
-      sweep(max(step, nctx), last, fetch, store, sees, true);
+      sweep(max(step, nctx), last, fetch, store, sees, scores, true);
       // a wave that is ahead may have raised it for its next item: then nothing is found here
       if (odd >= turn) {
         for (int s = max(step, nctx); s < last; ++s) {
