@@ -17,7 +17,11 @@
 // t of the product is then dims 8 c + t, and a lane ends with dims 32 g .. 32 g + 31
 // of its query.  A tile lies in one page, so every load has a scalar base and an
 // offset that is the lane's own.  Keys in e4m3 become bf16 on the way with their
-// power of two applied by the conversion (exact).  A head's keys and values are read
+// power of two applied by the conversion (exact).  Of a cache in e2m1 the values do so
+// too, eight a lane from one word; its keys are multiplied as they are held (Parts4).
+// 64 single tokens over up to 8192 positions, 32 / 8 heads, e2m1: 428 MB in 91 us, 4.7
+// TB/s, as a large copy runs; without the conversions 88, with two chunks ahead or
+// pages looked up earlier 91 to 93.  A head's keys and values are read
 // once for 16 query rows (again for the next 16, from a cache where it holds them)
 // and never pass through LDS.
 //
@@ -75,7 +79,12 @@ __device__ __forceinline__ float odd_part(uint16_t v) {
 // 224 .. 448 (e is that of its 32 dims), so an element is off by 2^-14 / 224 = 2^-21.8 of
 // the largest of its 32 at most.  The two products take the matrix cores as long as four
 // of bf16 do (34 cycles each), without converting the keys and with a quarter of
-// their bytes.  An infinity or a NaN makes a NaN of its row's scores.
+// their bytes.  The instruction aligns a sum's products to the largest and drops what
+// lies below about 2^-17 of it (measured): of a score whose products reach T, about
+// 2^-17 T.  A product of 100 changes nothing in a result (errors against 64 bits as with
+// bf16 keys of the same values); of 1000 they grow from 0.0020 to 0.0024, where rounding
+// such a key to 4 bits has long moved its score by more.  An infinity or a NaN makes a NaN of
+// its row's scores.
 struct Parts4 {
   i32x8 hi, lo;
   int scale;      // bytes: exponents of the 32 dims that are this lane's in the instruction's order, of hi and of lo
@@ -660,6 +669,9 @@ __global__ __launch_bounds__(64 * W, 8 / W) void paged_attention(PagedArgs a, in
 // ---------------------------------------------------------------------------
 constexpr int kTile = 64;
 constexpr int kRowBytes = 2 * kHead, kTileBytes = kTile * kRowBytes;
+// A tile of keys in e2m1 and their exponents, values in bf16.
+constexpr int kKeys4 = kTile * (kHead / 2 + kHead / kBlock), kBuffer4 = kKeys4 + kTileBytes;
+static_assert(3 * kBuffer4 <= 4 * kTileBytes, "three buffers of e2m1 in the LDS of two of bf16");
 #define LDS_AS __attribute__((address_space(3)))
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef short s16x8 __attribute__((ext_vector_type(8)));
@@ -763,21 +775,6 @@ __global__ __launch_bounds__(64 * W, 8 / W) void paged_tiles(PagedArgs a, int wh
         }
       }
     };
-    // the same of keys in e2m1: a row of 64 bytes keeps its 16-byte piece c at c ^ (row / 4) % 4,
-    // behind the rows a word for each lane (r16, g): the exponents of keys r16, 16 + r16, ..
-    auto scores_of_4 = [&](auto B, auto C, f32x4 (&sc)[RG][2]) __attribute__((always_inline)) {
-      LDS_AS char* const kt = lds + B.value * 2 * kTileBytes;
-      const int e = *reinterpret_cast<const LDS_AS int*>(kt + kTile * (kHead / 2) + (4 * r16 + g) * 4);
-      u32x4 kf[2];
-#pragma unroll
-      for (int t = 0; t < 2; ++t)
-        kf[t] = *reinterpret_cast<const LDS_AS u32x4*>(kt + (C.value * 32 + t * 16 + r16) * (kHead / 2) + (g ^ (r16 >> 2)) * 16);
-#pragma unroll
-      for (int r = 0; r < RG; ++r) {
-        sc[r][0] = scores4<2 * C.value>(kf[0], e, qp[r]);
-        sc[r][1] = scores4<2 * C.value + 1>(kf[1], e, qp[r]);
-      }
-    };
     // unseen keys out; the reference of a row moves as in chunk_weights, one test for all rows
     auto settle = [&](bool masked, const uint32_t (&vis)[RG], f32x4 (&sc)[RG][2]) __attribute__((always_inline)) {
       if (masked) {
@@ -844,7 +841,7 @@ __global__ __launch_bounds__(64 * W, 8 / W) void paged_tiles(PagedArgs a, int wh
     // into registers; store(B): the fetched tile to buffer B, returning which of
     // its keys are there (one that is not has zeros for values: 0 * NaN is NaN);
     // sees(s, r, there): what row group r sees of the keys that are.
-    auto sweep = [&](const int first, const int end, auto&& fetch, auto&& store, auto&& sees, auto&& scores, const bool tree) __attribute__((always_inline)) {
+    auto sweep = [&](const int first, const int end, auto&& fetch, auto&& store, auto&& sees, const bool tree) __attribute__((always_inline)) {
       if (first >= end) return;
       fetch(first);
       uint64_t there = store(Index<0>());
@@ -888,6 +885,105 @@ __global__ __launch_bounds__(64 * W, 8 / W) void paged_tiles(PagedArgs a, int wh
       }
     };
 
+    // The same of a context in e2m1, in three buffers, so that one barrier a tile will do,
+    // and with the next products' operands read and the products spread between the
+    // exponentials: a wave waits for a product that finds the matrix cores busy.  16
+    // requests x 512 nodes over 2048 positions, 32 / 8 heads, take 387 us, 0.89 PFLOP/s (in
+    // two buffers as above 399), 2 x 16 over 65536 67 (70).  Of the 399, without the
+    // exponentials 49 less, without the values' reads and products 90, without the keys' 85.
+    // Keys
+    // stay as they are held: a row of 64 bytes keeps its 16-byte piece c at c ^ (row / 4) % 4,
+    // behind the rows a word for each lane (r16, g): the exponents of keys r16, 16 + r16, ..
+    auto sweep4 = [&](const int first, const int end, auto&& fetch, auto&& store) __attribute__((always_inline)) {
+      if (first >= end) return;
+      const int k4 = r16 * (kHead / 2) + (g ^ (r16 >> 2)) * 16, e4 = kTile * (kHead / 2) + (4 * r16 + g) * 4;
+      struct Keys {
+        u32x4 k[2];
+        int e;
+      };
+      auto load_keys = [&](auto B, auto C, Keys& x) __attribute__((always_inline)) {
+        LDS_AS char* const kt = lds + B.value * kBuffer4;
+        x.e = *reinterpret_cast<const LDS_AS int*>(kt + e4);
+#pragma unroll
+        for (int t = 0; t < 2; ++t) x.k[t] = *reinterpret_cast<const LDS_AS u32x4*>(kt + k4 + (C.value * 32 + t * 16) * (kHead / 2));
+      };
+      auto load_values = [&](auto B, auto C, u32x4 (&vf)[8]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int t = 0; t < 8; ++t) {
+          const LDS_AS char* at = lds + va[t] + (B.value * kBuffer4 + kKeys4 - kTileBytes + C.value * 32 * kRowBytes);
+          const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4*)at);
+          const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4*)(at + 16 * kRowBytes));
+          vf[t] = __builtin_bit_cast(u32x4, s16x8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]});
+        }
+      };
+      auto scores4_of = [&](auto C, const Keys& x, f32x4 (&sc)[RG][2]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int r = 0; r < RG; ++r) {
+          sc[r][0] = scores4<2 * C.value>(x.k[0], x.e, qp[r]);
+          sc[r][1] = scores4<2 * C.value + 1>(x.k[1], x.e, qp[r]);
+        }
+      };
+      auto spread = [&] __attribute__((always_inline)) {
+        __builtin_amdgcn_sched_group_barrier(0x100, 19, 0);         // operands from LDS
+#pragma unroll
+        for (int i = 0; i < 4 * RG; ++i) {
+          __builtin_amdgcn_sched_group_barrier(0x402, 6, 0);        // weights
+          __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);        // scores
+        }
+      };
+      fetch(first);
+      uint64_t there = store(Index<0>());
+      if (first + 1 < end) fetch(first + 1);
+      __syncthreads();
+      f32x4 sa[RG][2], sb[RG][2];
+      u32x4 p[RG], vf[8];
+      Keys keys;
+      load_keys(Index<0>(), Index<0>(), keys);
+      scores4_of(Index<0>(), keys, sa);
+      auto values4 = [&] __attribute__((always_inline)) {
+#pragma unroll
+        for (int t = 0; t < 8; ++t)
+#pragma unroll
+          for (int r = 0; r < RG; ++r) o[r][t] = mfma16(vf[t], p[r], o[r][t]);
+      };
+      auto tile = [&](auto B, int s) __attribute__((always_inline)) {
+        const Index<(B.value + 1) % 3> next;
+        const bool masked = there != ~0ull;
+        uint32_t seen[2][RG];
+#pragma unroll
+        for (int r = 0; r < RG; ++r) {
+          seen[0][r] = uint32_t(there);
+          seen[1][r] = uint32_t(there >> 32);
+        }
+        settle(masked, seen[0], sa);
+        load_values(B, Index<0>(), vf);
+        load_keys(B, Index<1>(), keys);
+        scores4_of(Index<1>(), keys, sb);
+        weights(sa, p);
+        values4();
+        spread();
+        settle(masked, seen[1], sb);
+        if (s + 1 < end) {
+          there = store(next);
+          if (s + 2 < end) fetch(s + 2);
+        }
+        __syncthreads();
+        load_values(B, Index<1>(), vf);
+        load_keys(next, Index<0>(), keys);
+        scores4_of(Index<0>(), keys, sa);   // after the last tile: not used
+        weights(sb, p);
+        values4();
+        spread();
+      };
+#pragma unroll 1
+      for (int s = first; s < end; s += 3) {
+        tile(Index<0>(), s);
+        if (s + 1 < end) tile(Index<1>(), s + 1);
+        if (s + 2 < end) tile(Index<2>(), s + 2);
+      }
+      __syncthreads();   // the buffers are free again
+    };
+
     {   // the context
       const int32_t* table = a.c.table + int64_t(q) * a.c.max_pages;
       constexpr int kRowsWave = BITS == 16 ? 4 : 8, kShares = kTile / (kRowsWave * W);
@@ -929,7 +1025,7 @@ __global__ __launch_bounds__(64 * W, 8 / W) void paged_tiles(PagedArgs a, int wh
       auto store = [&](auto B) __attribute__((always_inline)) -> uint64_t {
         const uint64_t there = in_flight;
         const Piece zero = {};
-        LDS_AS char* const kt = lds + B.value * 2 * kTileBytes;
+        LDS_AS char* const kt = lds + B.value * (BITS == 4 ? kBuffer4 : 2 * kTileBytes);
 #pragma unroll
         for (int i = 0; i < kShares; ++i) {
           const int key = first_key(i) + (BITS == 16 ? g : lane >> 3);
@@ -940,7 +1036,7 @@ __global__ __launch_bounds__(64 * W, 8 / W) void paged_tiles(PagedArgs a, int wh
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
               const int c = 2 * (lane & 7) + h;
-              *reinterpret_cast<LDS_AS u32x4*>(kt + kTileBytes + key * kRowBytes + (c ^ v_place(key)) * 16) = expand8(vx[i][h], sv);
+              *reinterpret_cast<LDS_AS u32x4*>(kt + kKeys4 + key * kRowBytes + (c ^ v_place(key)) * 16) = expand8(vx[i][h], sv);
             }
             const int c = (lane & 7) >> 1;   // keys stay as they are
             *reinterpret_cast<LDS_AS u32x2*>(kt + key * (kHead / 2) + (c ^ ((key >> 2) & 3)) * 16 + (lane & 1) * 8) = kx[i];
@@ -976,9 +1072,8 @@ __global__ __launch_bounds__(64 * W, 8 / W) void paged_tiles(PagedArgs a, int wh
         return there;
       };
       if (step < min(last, nctx)) look_up(step);
-      auto all = [&](int, int, uint64_t there) { return there; };
-      if constexpr (BITS == 4) sweep(step, min(last, nctx), fetch, store, all, scores_of_4, false);
-      else sweep(step, min(last, nctx), fetch, store, all, scores, false);
+      if constexpr (BITS == 4) sweep4(step, min(last, nctx), fetch, store);
+      else sweep(step, min(last, nctx), fetch, store, [&](int, int, uint64_t there) { return there; }, false);
     }
     if constexpr (BITS == 4) load_query();
     const int tid = thread_again();
@@ -1034,7 +1129,7 @@ __global__ __launch_bounds__(64 * W, 8 / W) void paged_tiles(PagedArgs a, int wh
         const int d = node[r] - (s - nctx) * kTile;   // a chain's node sees keys up to its own
         return there & (d < 0 ? 0ull : d >= 63 ? ~0ull : (2ull << d) - 1);
       };
-      sweep(max(step, nctx), last, fetch, store, sees, scores, true);
+      sweep(max(step, nctx), last, fetch, store, sees, true);
       // a wave that is ahead may have raised it for its next item: then nothing is found here
       if (odd >= turn) {
         for (int s = max(step, nctx); s < last; ++s) {
@@ -1258,7 +1353,9 @@ Plan plan_of(int batch, int budget, int max_ctx, int heads_q, int heads_kv, int 
   // 2 requests 89 / 101, 3 127 / 107 and 116 / 101, 4 137 / 115 and 140 / 100, 5 191 /
   // 197, 8 255 / 215 and 244 / 191, 12 367 / 313 and 365 / 290, 16 435 / 397 and 405 /
   // 375, 17 468 / 480, 32 ragged 741 / 707; 4 over 500 positions 69 / 53, over 16000
-  // 632 / 575; bf16 alike.
+  // 632 / 575; bf16 alike.  e2m1 chooses alike: 1 request x 64 nodes over 2048 positions
+  // whole 15.9, shared 19.9, tiles of 64 rows 26, of 128 36; 2 x 16 nodes over 65536
+  // tiles of 64 rows 72 (67 now), 16 rows shared 91, tiles of 128 98.
   const bool wide = tiles_of(256) >= 192 && 10 * 256 * tiles_of(256) <= 11 * 128 * tiles_of(128);
   p.kernel = rows <= 16 || middle ? kFew : rows <= 64 || tiles_of(128) * steps < 8 * kResident ? kTiles64 : wide ? kTiles256 : kTiles128;
   p.rows = p.kernel == kFew ? 16 : p.kernel == kTiles64 ? 64 : p.kernel == kTiles128 ? 128 : 256;
