@@ -5,6 +5,11 @@
 // (their order does not matter: of two entries that name a page one finds its bit
 // set).  Needs and free pages are then numbered by prefix sums in ascending order,
 // so results do not depend on thread timing.
+//
+// What bounds them is latency: a launch (2.2 us each), the round trips start -> table
+// entry -> bitmap -> page, and a barrier or two a prefix sum.  64 requests of 4096
+// positions in pages of 64: fork 2.4 us, reserve 8.1 (as three launches 14.4).  A compact
+// of 8320 entries and 20000 pages 11 (as four launches 18).
 #include <algorithm>
 
 #include "internal.hpp"
@@ -36,6 +41,17 @@ __device__ __forceinline__ Space space_of(const PagesArgs& a) {
   return Space{w, w + words, upto, upto + padded(a.batch)};
 }
 
+// A small pool and table: one block does it all in one launch, bitmaps in LDS.  One
+// launch / clear, scan and the rest (us in a graph, entries of the table, pages):
+// reserve 4160, 4500 7.7 / 12.3; 16384, 18000 9.2 / 13.7; 32768, 35000 12.5 / 16.3;
+// 65536, 65000 17.5 / 17.7; 131072 25.6 / 18.3; compact 7.4 / 13.5; 12.8 / 17.2; 23.2 /
+// 23.6; 37.4 / 29.4.
+constexpr int kSmallPages = 65536, kSmallEntries = 32768;
+struct Bitmaps {
+  uint32_t named[kSmallPages / 32], shared[kSmallPages / 32];
+  int32_t before[kSmallPages / 32];   // compact's list
+};
+
 __device__ __forceinline__ bool is_page(int e, int num_pages) { return uint32_t(e) < uint32_t(num_pages); }
 
 __global__ __launch_bounds__(kThreads) void pages_fork(PagesArgs a) {
@@ -53,17 +69,38 @@ __global__ __launch_bounds__(kThreads) void pages_clear(PagesArgs a) {
     static_cast<uint32_t*>(a.ws)[i] = 0;
 }
 
-// Named and shared pages of the table, which is copied to `out` where that is another.
-__global__ __launch_bounds__(kThreads) void pages_scan(PagesArgs a) {
-  const Space s = space_of(a);
-  const int64_t n = int64_t(a.batch) * a.max_pages;
-  for (int64_t i = int64_t(blockIdx.x) * kThreads + threadIdx.x; i < n; i += int64_t(gridDim.x) * kThreads) {
-    const int e = a.table[i];
-    if (a.out != a.table) a.out[i] = e;
-    if (!is_page(e, a.num_pages)) continue;
-    const uint32_t bit = 1u << (e & 31);
-    if (atomicOr(s.named + (e >> 5), bit) & bit) atomicOr(s.shared + (e >> 5), bit);
+constexpr int kEach = 8;   // table entries of a thread that are loaded together
+
+// Named and shared pages of the table, which is copied to `out` where that is
+// another: thread t of n.
+__device__ __forceinline__ void scan(const PagesArgs& a, const Space& s, int64_t t, int64_t n) {
+  const int64_t items = int64_t(a.batch) * a.max_pages;
+  for (int64_t i0 = t; i0 < items; i0 += kEach * n) {
+    int e[kEach];
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) e[k] = i0 + k * n < items ? a.table[i0 + k * n] : -1;
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) {
+      if (a.out != a.table && i0 + k * n < items) a.out[i0 + k * n] = e[k];
+      if (!is_page(e[k], a.num_pages)) continue;
+      const uint32_t bit = 1u << (e[k] & 31);
+      if (atomicOr(s.named + (e[k] >> 5), bit) & bit) atomicOr(s.shared + (e[k] >> 5), bit);
+    }
   }
+}
+__global__ __launch_bounds__(kThreads) void pages_scan(PagesArgs a) {
+  scan(a, space_of(a), int64_t(blockIdx.x) * kThreads + threadIdx.x, int64_t(gridDim.x) * kThreads);
+}
+// The same by one block of a small table, into its LDS.
+__device__ __forceinline__ Space scan_small(const PagesArgs& a, Bitmaps* maps) {
+  Space s = space_of(a);
+  s.named = maps->named;
+  s.shared = maps->shared;
+  for (int w = threadIdx.x; w < words_of(a.num_pages); w += kWide) s.named[w] = s.shared[w] = 0;
+  __syncthreads();
+  scan(a, s, threadIdx.x, kWide);
+  __syncthreads();
+  return s;
 }
 
 // Exclusive prefix sums of x over the block's threads in order; total: of all.
@@ -116,17 +153,28 @@ __device__ __forceinline__ Need need_of(const PagesArgs& a, const uint32_t* shar
   return r;
 }
 
-// One block: the needs in order, the free pages in order, one to the other.
+// One block: the needs in order, the free pages in order, one to the other.  Up to
+// kWide items keep what they need in registers from the first pass to the last.
+template <bool SMALL>
 __global__ __launch_bounds__(kWide) void pages_reserve(PagesArgs a) {
-  const Space s = space_of(a);
+  Space s;
+  if constexpr (SMALL) {
+    __shared__ Bitmaps maps;
+    s = scan_small(a, &maps);
+  } else {
+    s = space_of(a);
+  }
+  const Need none{0, -1, false, false};
   const int64_t items = int64_t(a.batch) * a.columns;
-  int wanted = 0, total;
+  const bool once = items <= kWide;
+  Need need = none;
+  int wanted = 0, rank = 0, total;
   for (int64_t i0 = 0; i0 < items; i0 += kWide) {
     const int64_t i = i0 + threadIdx.x;
     const int q = int(i / a.columns), j = int(i - int64_t(q) * a.columns);
-    const Need n = i < items ? need_of(a, s.shared, q, j) : Need{0, -1, false, false};
-    const int before = block_prefix(n.page, &total);
-    if (i < items && j == a.columns - 1) s.upto[q] = wanted + before + n.page;
+    need = i < items ? need_of(a, s.shared, q, j) : none;
+    rank = wanted + block_prefix(need.page, &total);
+    if (i < items && j == a.columns - 1) s.upto[q] = rank + need.page;
     wanted += total;
   }
   const int words = words_of(a.num_pages);
@@ -135,8 +183,8 @@ __global__ __launch_bounds__(kWide) void pages_reserve(PagesArgs a) {
     const int w = w0 + threadIdx.x;
     uint32_t bits = w < words ? ~s.named[w] : 0u;
     if (w == words - 1 && (a.num_pages & 31)) bits &= (1u << (a.num_pages & 31)) - 1u;
-    int rank = free + block_prefix(__popc(bits), &total);
-    for (; bits && rank < wanted; bits &= bits - 1, ++rank) s.list[rank] = 32 * w + __builtin_ctz(bits);
+    int at = free + block_prefix(__popc(bits), &total);
+    for (; bits && at < wanted; bits &= bits - 1, ++at) s.list[at] = 32 * w + __builtin_ctz(bits);
     free += total;
   }
   __syncthreads();   // upto and list are written
@@ -144,35 +192,71 @@ __global__ __launch_bounds__(kWide) void pages_reserve(PagesArgs a) {
   for (int64_t i0 = 0; i0 < items; i0 += kWide) {
     const int64_t i = i0 + threadIdx.x;
     const int q = int(i / a.columns), j = int(i - int64_t(q) * a.columns);
-    Need n = i < items ? need_of(a, s.shared, q, j) : Need{0, -1, false, false};
+    if (!once) {
+      need = i < items ? need_of(a, s.shared, q, j) : none;
+      rank = pages + block_prefix(need.page, &total);
+      pages += total;
+    }
     const int upto = i < items ? s.upto[q] : 0;
     const bool granted = i < items && (upto <= free || upto == (q > 0 ? s.upto[q - 1] : 0));
-    const int rank = pages + block_prefix(n.page, &total);
-    pages += total;
-    if (!granted) n.page = n.copy = false;
-    const int place = copies + block_prefix(n.copy, &total);
+    const bool copy = granted && need.copy;
+    const int place = copies + block_prefix(copy, &total);
     copies += total;
-    block_prefix(n.page, &total);
-    taken += total;
-    if (n.page) {
+    if (granted && need.page) {
       const int to = s.list[rank];
-      a.out[n.at] = to;
-      if (n.copy) {
-        a.pairs[2 * int64_t(place)] = n.entry;
+      ++taken;
+      a.out[need.at] = to;
+      if (copy) {
+        a.pairs[2 * int64_t(place)] = need.entry;
         a.pairs[2 * int64_t(place) + 1] = to;
       }
     }
     if (i < items && j == 0) a.granted[q] = granted;
   }
+  block_prefix(taken, &total);
   if (threadIdx.x == 0) {
     a.totals[0] = copies;
-    a.totals[1] = free - taken;
+    a.totals[1] = free - total;
   }
 }
 
+// Table entries from `live` on become the pages that took theirs: thread t of n.
+__device__ __forceinline__ void remap(const PagesArgs& a, const Space& s, int live, int64_t t, int64_t n) {
+  const int64_t items = int64_t(a.batch) * a.max_pages;
+  for (int64_t i0 = t; i0 < items; i0 += kEach * n) {
+    int e[kEach];
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) e[k] = i0 + k * n < items ? a.table[i0 + k * n] : -1;
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) {
+      if (!is_page(e[k], a.num_pages)) {
+        e[k] = -1;
+      } else if (e[k] >= live) {
+        const int w = e[k] >> 5, first = max(live - 32 * w, 0);   // the word's pages below live stay
+        const uint32_t before = s.named[w] & ((1u << (e[k] & 31)) - 1u) & ~((1u << first) - 1u);
+        e[k] = a.pairs[2 * int64_t(s.list[w] + __popc(before)) + 1];
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < kEach; ++k)
+      if (i0 + k * n < items) a.out[i0 + k * n] = e[k];
+  }
+}
+__global__ __launch_bounds__(kThreads) void pages_remap(PagesArgs a) {
+  remap(a, space_of(a), a.totals[1], int64_t(blockIdx.x) * kThreads + threadIdx.x, int64_t(gridDim.x) * kThreads);
+}
+
 // One block: pages in use from `live` on to the free ones below it.
+template <bool SMALL>
 __global__ __launch_bounds__(kWide) void pages_compact(PagesArgs a) {
-  const Space s = space_of(a);
+  Space s;
+  if constexpr (SMALL) {
+    __shared__ Bitmaps maps;
+    s = scan_small(a, &maps);
+    s.list = maps.before;
+  } else {
+    s = space_of(a);
+  }
   const int words = words_of(a.num_pages);
   int live = 0, total;
   for (int w0 = 0; w0 < words; w0 += kWide) {
@@ -199,24 +283,13 @@ __global__ __launch_bounds__(kWide) void pages_compact(PagesArgs a) {
     a.totals[0] = from;
     a.totals[1] = live;
   }
-}
-
-__global__ __launch_bounds__(kThreads) void pages_remap(PagesArgs a) {
-  const Space s = space_of(a);
-  const int live = a.totals[1];
-  const int64_t n = int64_t(a.batch) * a.max_pages;
-  for (int64_t i = int64_t(blockIdx.x) * kThreads + threadIdx.x; i < n; i += int64_t(gridDim.x) * kThreads) {
-    int e = a.table[i];
-    if (!is_page(e, a.num_pages)) {
-      e = -1;
-    } else if (e >= live) {
-      const int w = e >> 5, first = max(live - 32 * w, 0);   // the word's pages below live stay
-      const uint32_t before = s.named[w] & ((1u << (e & 31)) - 1u) & ~((1u << first) - 1u);
-      e = a.pairs[2 * int64_t(s.list[w] + __popc(before)) + 1];
-    }
-    a.out[i] = e;
+  if constexpr (SMALL) {
+    __syncthreads();   // pairs and list are written
+    remap(a, s, live, threadIdx.x, kWide);
   }
 }
+
+bool is_small(const PagesArgs& a) { return a.num_pages <= kSmallPages && int64_t(a.batch) * a.max_pages <= kSmallEntries; }
 
 unsigned blocks_for(int64_t items) { return unsigned(std::min<int64_t>(2048, (items + kThreads - 1) / kThreads)); }
 
@@ -226,7 +299,9 @@ hipError_t launch_scan(const PagesArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
-// A unit of the copy: 16 KB of a page's keys or values, or a page's exponents.
+// A unit of the copy: 16 KB of a page's keys or values, or a page's exponents; a
+// thread has four loads of 16 bytes in flight.  Bound by memory: 512 MB read and
+// written (compact) in 92 us, 5.6 TB/s; 134 MB in 13.5, as far as the caches hold them.
 constexpr int kUnit = 16384;
 __global__ __launch_bounds__(kThreads) void cache_copy(PageCopyArgs a) {
   const int pairs = min(a.count[0], a.max_pairs);
@@ -272,16 +347,24 @@ hipError_t launch_pages_fork(const PagesArgs& a, hipStream_t s) {
 }
 
 hipError_t launch_pages_reserve(const PagesArgs& a, hipStream_t s) {
+  if (is_small(a)) {
+    hipLaunchKernelGGL(pages_reserve<true>, dim3(1), dim3(kWide), 0, s, a);
+    return hipGetLastError();
+  }
   const hipError_t e = launch_scan(a, s);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(pages_reserve, dim3(1), dim3(kWide), 0, s, a);
+  hipLaunchKernelGGL(pages_reserve<false>, dim3(1), dim3(kWide), 0, s, a);
   return hipGetLastError();
 }
 
 hipError_t launch_pages_compact(const PagesArgs& a, hipStream_t s) {
+  if (is_small(a)) {
+    hipLaunchKernelGGL(pages_compact<true>, dim3(1), dim3(kWide), 0, s, a);
+    return hipGetLastError();
+  }
   const hipError_t e = launch_scan(a, s);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(pages_compact, dim3(1), dim3(kWide), 0, s, a);
+  hipLaunchKernelGGL(pages_compact<false>, dim3(1), dim3(kWide), 0, s, a);
   hipLaunchKernelGGL(pages_remap, dim3(blocks_for(int64_t(a.batch) * a.max_pages)), dim3(kThreads), 0, s, a);
   return hipGetLastError();
 }
