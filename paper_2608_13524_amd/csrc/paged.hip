@@ -886,14 +886,16 @@ __global__ __launch_bounds__(64 * W, 8 / W) void paged_tiles(PagedArgs a, int wh
     };
 
     // The same of a context in e2m1, in three buffers, so that one barrier a tile will do,
-    // and with the next products' operands read and the products spread between the
-    // exponentials: a wave waits for a product that finds the matrix cores busy.  16
-    // requests x 512 nodes over 2048 positions, 32 / 8 heads, take 387 us, 0.89 PFLOP/s (in
-    // two buffers as above 399), 2 x 16 over 65536 67 (70).  Of the 399, without the
-    // exponentials 49 less, without the values' reads and products 90, without the keys' 85.
-    // Keys
-    // stay as they are held: a row of 64 bytes keeps its 16-byte piece c at c ^ (row / 4) % 4,
-    // behind the rows a word for each lane (r16, g): the exponents of keys r16, 16 + r16, ..
+    // with the next tile stored first of all, the next products' operands read and the products
+    // spread between the exponentials (a wave waits for a product that finds the matrix cores
+    // busy), and the values' products ahead of the other wave of a SIMD, which has
+    // exponentials to do.  16 requests x 512 nodes over 2048 positions, 32 / 8 heads (us): in two
+    // buffers as above 399, in three 387, with the store first and the priority 356
+    // (345 in a graph, 1.0 PFLOP/s; e4m3 388); 2 x 16 nodes over 65536 70, 67, 64.  Of the
+    // 399, without the exponentials 49 less, without the values' reads and products 90,
+    // without the keys' 85.  Keys stay as they are held: a row of 64 bytes keeps its 16-byte
+    // piece c at c ^ (row / 4) % 4, behind the rows a word for each lane (r16, g): the
+    // exponents of keys r16, 16 + r16, ..
     auto sweep4 = [&](const int first, const int end, auto&& fetch, auto&& store) __attribute__((always_inline)) {
       if (first >= end) return;
       const int k4 = r16 * (kHead / 2) + (g ^ (r16 >> 2)) * 16, e4 = kTile * (kHead / 2) + (4 * r16 + g) * 4;
@@ -941,10 +943,12 @@ __global__ __launch_bounds__(64 * W, 8 / W) void paged_tiles(PagedArgs a, int wh
       load_keys(Index<0>(), Index<0>(), keys);
       scores4_of(Index<0>(), keys, sa);
       auto values4 = [&] __attribute__((always_inline)) {
+        __builtin_amdgcn_s_setprio(1);
 #pragma unroll
         for (int t = 0; t < 8; ++t)
 #pragma unroll
           for (int r = 0; r < RG; ++r) o[r][t] = mfma16(vf[t], p[r], o[r][t]);
+        __builtin_amdgcn_s_setprio(0);
       };
       auto tile = [&](auto B, int s) __attribute__((always_inline)) {
         const Index<(B.value + 1) % 3> next;
@@ -955,6 +959,10 @@ __global__ __launch_bounds__(64 * W, 8 / W) void paged_tiles(PagedArgs a, int wh
           seen[0][r] = uint32_t(there);
           seen[1][r] = uint32_t(there >> 32);
         }
+        if (s + 1 < end) {
+          there = store(next);
+          if (s + 2 < end) fetch(s + 2);
+        }
         settle(masked, seen[0], sa);
         load_values(B, Index<0>(), vf);
         load_keys(B, Index<1>(), keys);
@@ -963,10 +971,6 @@ __global__ __launch_bounds__(64 * W, 8 / W) void paged_tiles(PagedArgs a, int wh
         values4();
         spread();
         settle(masked, seen[1], sb);
-        if (s + 1 < end) {
-          there = store(next);
-          if (s + 2 < end) fetch(s + 2);
-        }
         __syncthreads();
         load_values(B, Index<1>(), vf);
         load_keys(next, Index<0>(), keys);
@@ -1355,7 +1359,7 @@ Plan plan_of(int batch, int budget, int max_ctx, int heads_q, int heads_kv, int 
   // 375, 17 468 / 480, 32 ragged 741 / 707; 4 over 500 positions 69 / 53, over 16000
   // 632 / 575; bf16 alike.  e2m1 chooses alike: 1 request x 64 nodes over 2048 positions
   // whole 15.9, shared 19.9, tiles of 64 rows 26, of 128 36; 2 x 16 nodes over 65536
-  // tiles of 64 rows 72 (67 now), 16 rows shared 91, tiles of 128 98.
+  // tiles of 64 rows 72 (64 now), 16 rows shared 91, tiles of 128 98.
   const bool wide = tiles_of(256) >= 192 && 10 * 256 * tiles_of(256) <= 11 * 128 * tiles_of(128);
   p.kernel = rows <= 16 || middle ? kFew : rows <= 64 || tiles_of(128) * steps < 8 * kResident ? kTiles64 : wide ? kTiles256 : kTiles128;
   p.rows = p.kernel == kFew ? 16 : p.kernel == kTiles64 ? 64 : p.kernel == kTiles128 ? 128 : 256;
