@@ -1013,12 +1013,12 @@ __global__ __launch_bounds__(64 * W, 8 / W) void paged_tiles(PagedArgs a, int wh
           const int of = __builtin_amdgcn_readlane(page, first_key(i) >> 4);
           const int64_t in = uint32_t(of) < uint32_t(a.c.num_pages) ? of : 0;   // any page: what is read is not used
           const int64_t row0 = ((in * a.heads_kv + kvh) << a.c.page_log2) + ((kb + first_key(i)) & page_mask);
-          const int64_t byte0 = row0 * (kHead * BITS / 8) + int64_t(sizeof(Piece)) * lane;
-          kx[i] = *reinterpret_cast<const Piece*>(static_cast<const char*>(a.c.k) + byte0);
-          vx[i] = *reinterpret_cast<const Piece*>(static_cast<const char*>(a.c.v) + byte0);
+          const int64_t byte0 = row0 * (kHead * BITS / 8);
+          kx[i] = *reinterpret_cast<const Piece*>(static_cast<const char*>(a.c.k) + byte0 + int(sizeof(Piece)) * lane);
+          vx[i] = *reinterpret_cast<const Piece*>(static_cast<const char*>(a.c.v) + byte0 + int(sizeof(Piece)) * lane);
           if constexpr (BITS == 4) {   // a lane's 16 elements lie in one block
-            ke[i] = a.c.k_exp[row0 * (kHead / kBlock) + (lane >> 1)];
-            ve[i] = a.c.v_exp[row0 * (kHead / kBlock) + (lane >> 1)];
+            ke[i] = (a.c.k_exp + row0 * (kHead / kBlock))[lane >> 1];
+            ve[i] = (a.c.v_exp + row0 * (kHead / kBlock))[lane >> 1];
           } else if constexpr (BITS == 8) {
             ke[i] = a.c.k_exp[row0 + (lane >> 3)];
             ve[i] = a.c.v_exp[row0 + (lane >> 3)];

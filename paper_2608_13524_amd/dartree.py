@@ -607,7 +607,7 @@ def _place(stream):
     import torch
     if not torch.cuda.is_initialized():
         return -1, None
-    device = torch.cuda.current_device()
+    device = torch._C._cuda_getDevice()   # as current_device() once the GPU is in use, without its check for that
     if stream is None:   # the handle itself: making a Stream object of it takes 2.7 us, a short call's kernel 3
         return device, torch._C._cuda_getCurrentRawStream(device)
     if getattr(stream, "device_index", device) != device:
@@ -693,11 +693,11 @@ class DeviceCache:
     def _layout(p: CacheParams):
         """(dtype, shape of k and v, shape of the exponents or None)."""
         import torch
-        shape = (p.num_pages, p.heads_kv, p.page)
-        if p.type == CACHE_E2M1:
-            return torch.uint8, (*shape, p.head_dim // 2), (*shape, p.head_dim // 32)
-        if p.type == CACHE_E4M3:
+        shape, kind = (p.num_pages, p.heads_kv, p.page), p.type
+        if kind == CACHE_E4M3:
             return torch.float8_e4m3fn, (*shape, p.head_dim), shape
+        if kind == CACHE_E2M1:
+            return torch.uint8, (*shape, p.head_dim // 2), (*shape, p.head_dim // 32)
         return torch.bfloat16, (*shape, p.head_dim), None
 
     def checked(self, p: CacheParams, where: str, device: int) -> CacheC:

@@ -6,7 +6,9 @@ that differs, queries multiplied in two e4m3 parts under a power of two for each
 of them, leaves at most 2^-21 of the largest of those 32 of an element (the second
 part has 4 bits of what the first leaves, down to 2^-13 where the largest is held
 above 2^7): 128 such errors in a score of the sizes here, below 2^-12 of its absolute
-sum, lie within the 2^-10 that are allowed for weights there."""
+sum, lie within the 2^-10 that are allowed for weights there.  So does what the matrix
+instruction drops of a score's products, 2^-17 of the largest of them each: 2^-17 of
+a few units here."""
 import numpy as np
 import pytest
 import torch
