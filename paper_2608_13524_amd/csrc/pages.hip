@@ -9,7 +9,7 @@
 // What bounds them is latency: a launch (2.2 us each), the round trips start -> table
 // entry -> bitmap -> page, and a barrier or two a prefix sum.  64 requests of 4096
 // positions in pages of 64: fork 2.4 us, reserve 8.1 (as three launches 14.4).  A compact
-// of 8320 entries and 20000 pages 11 (as four launches 18).
+// of a table of 8320 entries and as many pages 11 (as four launches 18).
 #include <algorithm>
 
 #include "internal.hpp"
