@@ -4,7 +4,7 @@
 //
 // A row is 16 lanes of 8 elements (16 bytes of bf16, 8 of e4m3, 4 of e2m1); a lane moves
 // its eighth of the key and of the value row of one (request, position, head),
-// heads fastest, so that a wave reads 1 KB of consecutive source bytes and
+// heads fastest (but see Move), so that a wave reads 1 KB of consecutive source bytes and
 // writes whole rows of 256, 128 or 64 bytes.  A power of two as scale costs nothing:
 // e4m3 is a floating type, its rounding is relative, and scaling by a power of
 // two is exact, so the bytes are the nearest ones to x 2^-e whatever the order
@@ -12,7 +12,7 @@
 //
 // e2m1 has one bit of mantissa and two of exponent, so a power of two serves 32 elements,
 // four lanes.  Bound by memory: a ragged batch of 8 x 2048 positions of 8 heads is written
-// in 16 us and read in 16 (63 MB each, 4 TB/s); 16 x 16 in 3.6 and 3.4, the launch.  Two rows a
+// and read in 28 us (127 MB, 4.5 TB/s); 16 x 16 in 3.6 and 3.4, the launch.  Two rows a
 // thread, their loads in flight together, take as long.
 #include "reduce.hpp"
 #include "serve.hpp"
@@ -29,6 +29,33 @@ __device__ __forceinline__ int64_t slot_of(const CacheView& c, int q, int64_t po
   const int page = c.table[int64_t(q) * c.max_pages + (pos >> c.page_log2)];
   if (page < 0 || page >= c.num_pages) return -1;
   return ((int64_t(page) * c.heads_kv) << c.page_log2) + (pos & ((1 << c.page_log2) - 1));
+}
+
+// What 16 lanes move: head `head` of row i of request q; r: its place in [q][i][head].
+// A block's 16 are consecutive heads and rows, but in e2m1, where a row of the cache is half
+// a line of 128 bytes, 16 positions of one head, so that no line is written or read by
+// blocks of two XCDs (us, write / read of 8 x 2048 positions of 8 heads 17.0 / 15.9 -> 16.1 /
+// 14.9, 8 x 8192 68 / 67 -> 64 / 61; e4m3 18 / 17 either way, bf16 99 / 93 -> 105 / 102).
+struct Move {
+  int q, i, head;
+  unsigned r;   // below 2^31
+};
+template <int BITS>
+__host__ __device__ __forceinline__ bool by_positions(const CacheMoveArgs& a) {
+  return BITS == 4 && a.rows >= 16;
+}
+template <int BITS>
+__device__ __forceinline__ bool move_of(const CacheMoveArgs& a, Move* m) {
+  const unsigned heads = unsigned(a.c.heads_kv), rows = unsigned(a.rows), part = threadIdx.x >> 4;
+  if (by_positions<BITS>(a)) {
+    const unsigned tiles = (rows + 15) / 16, tile = blockIdx.x / heads, q = tile / tiles, i = (tile - q * tiles) * 16 + part;
+    const unsigned head = blockIdx.x - tile * heads;
+    *m = Move{int(q), int(i), int(head), (q * rows + i) * heads + head};
+    return i < rows;
+  }
+  const unsigned r = blockIdx.x * 16 + part, qi = r / heads, q = qi / rows;
+  *m = Move{int(q), int(qi - q * rows), int(r - qi * heads), r};
+  return int(q) < a.c.batch;
 }
 
 __device__ __forceinline__ float low(uint32_t w) { return __uint_as_float(w << 16); }
@@ -95,14 +122,12 @@ __device__ __forceinline__ u32x2 quantise(u32x4 x, int& e) {
 
 template <int BITS>
 __global__ __launch_bounds__(256) void cache_write(CacheMoveArgs a) {
-  const unsigned r = blockIdx.x * 16 + (threadIdx.x >> 4);   // below 2^31
   const int lane = threadIdx.x & 15;
-  const int head = int(r % unsigned(a.c.heads_kv));
-  const unsigned qi = r / unsigned(a.c.heads_kv);
-  const int q = int(qi / unsigned(a.rows)), i = int(qi % unsigned(a.rows));
-  if (q >= a.c.batch) return;
+  Move m;
+  if (!move_of<BITS>(a, &m)) return;
+  const int q = m.q, i = m.i, head = m.head;
   const int n = a.counts ? a.counts[q] : a.rows;
-  const int src = a.index ? a.index[qi] : i;
+  const int src = a.index ? a.index[int64_t(q) * a.rows + i] : i;
   const int64_t slot = slot_of(a.c, q, int64_t(a.start ? a.start[q] : 0) + i);
   if (i >= n || src < 0 || src >= a.source_rows || slot < 0) return;   // the same for a row's 16 lanes
   const int64_t at = (int64_t(q) * a.source_rows + src) * a.row_stride + head * kHead + lane * 8;
@@ -146,12 +171,10 @@ __device__ __forceinline__ u32x4 expand(u32x2 x, uint32_t e) {
 
 template <int BITS>
 __global__ __launch_bounds__(256) void cache_read(CacheMoveArgs a) {
-  const unsigned r = blockIdx.x * 16 + (threadIdx.x >> 4);   // below 2^31
   const int lane = threadIdx.x & 15;
-  const int head = int(r % unsigned(a.c.heads_kv));
-  const unsigned qi = r / unsigned(a.c.heads_kv);
-  const int q = int(qi / unsigned(a.rows)), i = int(qi % unsigned(a.rows));
-  if (q >= a.c.batch) return;
+  Move m;
+  if (!move_of<BITS>(a, &m)) return;
+  const int q = m.q, i = m.i, head = m.head;
   if (a.counts && i >= a.counts[q]) return;
   const int64_t slot = slot_of(a.c, q, int64_t(a.start ? a.start[q] : 0) + i);
   u32x4 k{0, 0, 0, 0}, v{0, 0, 0, 0};
@@ -182,27 +205,36 @@ __global__ __launch_bounds__(256) void cache_read(CacheMoveArgs a) {
       v = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(a.c.v) + from);
     }
   }
-  const int64_t to = int64_t(r) * kHead + lane * 8;   // [q][i][head]
+  const int64_t to = int64_t(m.r) * kHead + lane * 8;   // [q][i][head]
   *reinterpret_cast<u32x4*>(a.k_out + to) = k;
   *reinterpret_cast<u32x4*>(a.v_out + to) = v;
 }
 
+template <int BITS>
 unsigned blocks_of(const CacheMoveArgs& a) {
+  if (by_positions<BITS>(a)) return unsigned(int64_t(a.c.batch) * ((a.rows + 15) / 16) * a.c.heads_kv);
   return unsigned((int64_t(a.c.batch) * a.rows * a.c.heads_kv + 15) / 16);
+}
+
+template <int BITS>
+hipError_t launch_write(const CacheMoveArgs& a, hipStream_t s) {
+  hipLaunchKernelGGL(cache_write<BITS>, dim3(blocks_of<BITS>(a)), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+template <int BITS>
+hipError_t launch_read(const CacheMoveArgs& a, hipStream_t s) {
+  hipLaunchKernelGGL(cache_read<BITS>, dim3(blocks_of<BITS>(a)), dim3(256), 0, s, a);
+  return hipGetLastError();
 }
 
 }  // namespace
 
 hipError_t launch_cache_write(const CacheMoveArgs& a, hipStream_t s) {
-  auto* kernel = a.bits == 4 ? cache_write<4> : a.bits == 8 ? cache_write<8> : cache_write<16>;
-  hipLaunchKernelGGL(kernel, dim3(blocks_of(a)), dim3(256), 0, s, a);
-  return hipGetLastError();
+  return a.bits == 4 ? launch_write<4>(a, s) : a.bits == 8 ? launch_write<8>(a, s) : launch_write<16>(a, s);
 }
 
 hipError_t launch_cache_read(const CacheMoveArgs& a, hipStream_t s) {
-  auto* kernel = a.bits == 4 ? cache_read<4> : a.bits == 8 ? cache_read<8> : cache_read<16>;
-  hipLaunchKernelGGL(kernel, dim3(blocks_of(a)), dim3(256), 0, s, a);
-  return hipGetLastError();
+  return a.bits == 4 ? launch_read<4>(a, s) : a.bits == 8 ? launch_read<8>(a, s) : launch_read<16>(a, s);
 }
 
 }  // namespace dartree
