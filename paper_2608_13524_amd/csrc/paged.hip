@@ -784,8 +784,12 @@ __global__ __launch_bounds__(64 * W, 8 / W) void paged_tiles(PagedArgs a, int wh
 #pragma unroll
           for (int t = 0; t < 2; ++t)
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-              if (!((bits >> (16 * t + i)) & 1u)) sc[r][t][i] = -INFINITY;
+            for (int i = 0; i < 4; ++i) {
+              // two instructions a score, the bit to all bits and a choice by them (a test takes
+              // three: 147 -> 143 us for 16 x 512 nodes without a context)
+              const uint32_t keep = uint32_t(__builtin_amdgcn_sbfe(int(bits), 16 * t + i, 1));
+              sc[r][t][i] = __uint_as_float((__float_as_uint(sc[r][t][i]) & keep) | (0xFF800000u & ~keep));
+            }
         }
       }
       float top[RG];
@@ -890,8 +894,8 @@ __global__ __launch_bounds__(64 * W, 8 / W) void paged_tiles(PagedArgs a, int wh
     // spread between the exponentials (a wave waits for a product that finds the matrix cores
     // busy), and the values' products ahead of the other wave of a SIMD, which has
     // exponentials to do.  16 requests x 512 nodes over 2048 positions, 32 / 8 heads (us): in two
-    // buffers as above 399, in three 387, with the store first and the priority 356
-    // (345 in a graph, 1.0 PFLOP/s; e4m3 388); 2 x 16 nodes over 65536 70, 67, 64.  Of the
+    // buffers as above 399, in three 387, with the store first and the priority 353
+    // (344 in a graph, 1.0 PFLOP/s; e4m3 376); 2 x 16 nodes over 65536 70, 67, 64.  Of the
     // 399, without the exponentials 49 less, without the values' reads and products 90,
     // without the keys' 85.  Keys stay as they are held: a row of 64 bytes keeps its 16-byte
     // piece c at c ^ (row / 4) % 4, behind the rows a word for each lane (r16, g): the
