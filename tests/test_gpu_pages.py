@@ -34,7 +34,8 @@ def random_table(rng, b, columns, num_pages, named=0.5, shared=0.2):
 
 
 SHAPES = [(1, 1, 1), (1, 3, 2), (2, 5, 33), (7, 13, 64), (3, 1, 5), (64, 40, 3000), (1, 2000, 2500), (300, 9, 70000), (1500, 3, 100),
-          (2, 70000, 300000), (5, 33, 1024), (128, 128, 65536), (128, 128, 65537), (182, 181, 20000)]
+          (2, 70000, 300000), (5, 33, 1024), (128, 128, 65536), (128, 128, 65537), (182, 181, 20000), (1024, 1, 2000),
+          (1025, 1, 900)]
 
 
 def run_reserve(p, table, rows, start, counts, place="apart", source=None):
