@@ -972,14 +972,20 @@ def rotary(p: RotaryParams, turns, q, k, q_out, k_out, positions=None, start=Non
     import torch
     where, i32 = "rotary", torch.int32
     device, st = _place(stream)
-    b, rows = p.batch, p.rows
+    b, rows, hq, hkv, d = p.batch, p.rows, p.heads_q, p.heads_kv, p.head_dim
     dtypes = (torch.bfloat16,) if p.type == BF16 else (torch.float32,)
-    args = []
-    for name, x, heads in (("q", q, p.heads_q), ("k", k, p.heads_kv), ("q_out", q_out, p.heads_q), ("k_out", k_out, p.heads_kv)):
-        args += [None, 0] if heads == 0 else _rows(where, name, x, dtypes, (b, rows, heads, p.head_dim), device)
+    qp, qs = qo, qos = kp, ks = ko, kos = None, 0
+    if hq:
+        shape = (b, rows, hq, d)
+        qp, qs = _rows(where, "q", q, dtypes, shape, device)
+        qo, qos = _rows(where, "q_out", q_out, dtypes, shape, device)
+    if hkv:
+        shape = (b, rows, hkv, d)
+        kp, ks = _rows(where, "k", k, dtypes, shape, device)
+        ko, kos = _rows(where, "k_out", k_out, dtypes, shape, device)
     tp = _dense(where, "turns", turns, torch.int64, (p.rotary_dim // 2,), device)
     pp = _dense(where, "positions", positions, i32, (b, rows), device)
     sp = _dense(where, "start", start, i32, (b,), device)
     cp = _dense(where, "counts", counts, i32, (b,), device)
     _on_device(where, device)
-    _check(lib().dartree_rotary(ctypes.byref(p), tp, *args, pp, sp, cp, st), "dartree_rotary")
+    _check(lib().dartree_rotary(ctypes.byref(p), tp, qp, qs, kp, ks, qo, qos, ko, kos, pp, sp, cp, st), "dartree_rotary")
