@@ -12,7 +12,7 @@
 //
 // e2m1 has one bit of mantissa and two of exponent, so a power of two serves 32 elements,
 // four lanes.  Bound by memory: a ragged batch of 8 x 2048 positions of 8 heads is written
-// and read in 28 us (127 MB, 4.5 TB/s); 16 x 16 in 3.6 and 3.4, the launch.  Two rows a
+// and read in 28 us (127 MB, 4.5 TB/s); 16 x 16 in 3.2 and 3.1, the launch.  Two rows a
 // thread, their loads in flight together, take as long.
 #include "reduce.hpp"
 #include "serve.hpp"
