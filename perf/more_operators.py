@@ -518,8 +518,7 @@ def _plain_reserve(s):
     shared = touched & there & (holders[table.clamp(0, n - 1).long()] > 1)
     need = shared | (touched & ~there)
     free = (holders[:n] == 0).sum()
-    wanted = need.sum(dim=1)
-    granted = (wanted == 0) | (wanted.cumsum(0) <= free)   # in order, as far as pages go
+    granted = need.sum(dim=1).cumsum(0) <= free
     need &= granted[:, None]
     lowest = torch.argsort((holders[:n] > 0).to(torch.int8), stable=True)   # free pages first, ascending
     rank = need.flatten().cumsum(0).view(b, -1) - 1
