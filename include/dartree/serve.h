@@ -121,9 +121,7 @@ dartree_status dartree_tree_attention_paged_workspace_size(const dartree_attn_pa
  * heads_q * 128 each; k_tree, v_tree: likewise with kv_stride and heads_kv;
  * strides are multiples of 8.  out: bf16 [b][budget][heads_q][128].
  * Products of bf16 values (e4m3 and e2m1 keys and values as dartree_cache_read gives
- * them) with fp32 accumulation, fp32 softmax; over e2m1 keys an element of a query is
- * taken to 2^-21 of the largest of its 32, and each product of a score to about 2^-17
- * of the largest of them (far less than 4 bits have rounded that key by); the weights are rounded to bf16 for
+ * them) with fp32 accumulation, fp32 softmax; the weights are rounded to bf16 for
  * the weighted sum of values, the output to bf16.  Weights are at most 2^8 before
  * they are divided by their sum: values below 2^89 cannot overflow it.  The order
  * of sums is fixed by the arguments: equal calls give equal bits. */

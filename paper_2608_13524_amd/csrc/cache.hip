@@ -61,6 +61,13 @@ __device__ __forceinline__ bool move_of(const CacheMoveArgs& a, Move* m) {
 __device__ __forceinline__ float low(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float high(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
 
+// Least e >= kExpLow with amax <= 448 * 2^e = 1.75 * 2^(e + 8).
+__device__ __forceinline__ int row_exponent(float amax) {
+  const uint32_t u = __float_as_uint(amax);
+  const int e = int(u >> 23) - 127 - 8 + ((u & 0x7FFFFFu) > 0x600000u);
+  return min(max(e, kExpLow), 120);
+}
+
 // Least e >= kExpLow with amax <= 6 * 2^e = 1.5 * 2^(e + 2).  At most 125: 6 * 2^126
 // is no bf16 number, so the numbers above 6 * 2^125 are held as that.
 __device__ __forceinline__ int block_exponent(float amax) {

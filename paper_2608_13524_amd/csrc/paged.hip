@@ -17,8 +17,8 @@
 // t of the product is then dims 8 c + t, and a lane ends with dims 32 g .. 32 g + 31
 // of its query.  A tile lies in one page, so every load has a scalar base and an
 // offset that is the lane's own.  Keys in e4m3 become bf16 on the way with their
-// power of two applied by the conversion (exact).  Of a cache in e2m1 the values do so
-// too, eight a lane from one word; its keys are multiplied as they are held (Parts4).
+// power of two applied by the conversion (exact), and so do those in e2m1, eight from a
+// word.
 // 64 single tokens over up to 8192 positions, 32 / 8 heads, e2m1: 428 MB in 91 us, 4.7
 // TB/s, as a large copy runs; without the conversions 88, with two chunks ahead or
 // pages looked up earlier 91 to 93.  A head's keys and values are read
@@ -36,7 +36,6 @@ namespace dartree {
 namespace {
 
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-typedef int i32x8 __attribute__((ext_vector_type(8)));
 
 constexpr int kChunk = 32;            // keys of a wave's share of a step
 
@@ -70,71 +69,6 @@ __device__ __forceinline__ uint32_t without_odd(uint32_t w) {
 }
 __device__ __forceinline__ float odd_part(uint16_t v) {
   return (v & 0x7F80u) == 0x7F80u ? __uint_as_float(uint32_t(v) << 16) : 0.f;
-}
-
-// A query's row for products with keys in e2m1, which the matrix instruction takes as
-// they are, 128 dims at once, with the exponent byte of each 32.  Its other operand is
-// 8 bits wide, so a query goes in two parts, e4m3 of q 2^-e and e4m3 of 2^4 times what
-// that leaves: 4 + 4 bits hold the 8 of a bf16 number, down to 2^-13 under a largest of
-// 224 .. 448 (e is that of its 32 dims), so an element is off by 2^-14 / 224 = 2^-21.8 of
-// the largest of its 32 at most.  The two products take the matrix cores as long as four
-// of bf16 do (34 cycles each), without converting the keys and with a quarter of
-// their bytes.  The instruction aligns a sum's products to the largest and drops what
-// lies below about 2^-17 of it (measured): of a score whose products reach T, about
-// 2^-17 T.  A product of 100 changes nothing in a result (errors against 64 bits as with
-// bf16 keys of the same values); of 1000 they grow from 0.0020 to 0.0024, where rounding
-// such a key to 4 bits has long moved its score by more.  An infinity or a NaN makes a NaN of
-// its row's scores.
-struct Parts4 {
-  i32x8 hi, lo;
-  int scale;      // bytes: exponents of the 32 dims that are this lane's in the instruction's order, of hi and of lo
-};
-__device__ __forceinline__ Parts4 query_parts(const uint16_t* q) {
-  typedef float f32x2 __attribute__((ext_vector_type(2)));
-  const int lane = threadIdx.x & 63, g = lane >> 4;
-  Parts4 r;
-  int e[2];   // a lane has dims 16 g .. + 15 and 64 + 16 g .. + 15
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    float f[16], m = 0.f;
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const u32x4 x = *reinterpret_cast<const u32x4*>(q + 64 * h + 16 * g + 8 * i);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        f[8 * i + 2 * j] = __uint_as_float(x[j] << 16);
-        f[8 * i + 2 * j + 1] = __uint_as_float(x[j] & 0xFFFF0000u);
-        m = fmaxf(m, fmaxf(fabsf(f[8 * i + 2 * j]), fabsf(f[8 * i + 2 * j + 1])));
-      }
-    }
-    m = fmaxf(m, __shfl_xor(m, 16));
-    e[h] = row_exponent<-122>(m);   // as low as the exponent byte of lo goes: the least normal numbers keep their bits
-    const float s = __uint_as_float(uint32_t(127 - e[h]) << 23);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float a = f[4 * i] * s, b = f[4 * i + 1] * s, c = f[4 * i + 2] * s, d = f[4 * i + 3] * s;
-      int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
-      w = __builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
-      const f32x2 ab = __builtin_amdgcn_cvt_pk_f32_fp8(w, false), cd = __builtin_amdgcn_cvt_pk_f32_fp8(w, true);
-      int v = __builtin_amdgcn_cvt_pk_fp8_f32((a - ab[0]) * 16.f, (b - ab[1]) * 16.f, 0, false);
-      v = __builtin_amdgcn_cvt_pk_fp8_f32((c - cd[0]) * 16.f, (d - cd[1]) * 16.f, v, true);
-      r.hi[4 * h + i] = w;
-      r.lo[4 * h + i] = v;
-    }
-  }
-  const int of = (lane & 15) + 32 * (g & 1);   // dims 32 g .. + 31 are halves g / 2 of lane groups 2 (g % 2) and the next
-  const int e0 = __shfl(e[0], of), e1 = __shfl(e[1], of);
-  const int own = (g < 2 ? e0 : e1) + 127;
-  r.scale = own | ((own - 4) << 8);
-  return r;
-}
-// Scores of 16 keys; byte T of `scale`: the exponent of the key's 32 dims.
-template <int T>
-__device__ __forceinline__ f32x4 scores4(u32x4 k, int scale, const Parts4& q) {
-  const i32x8 a{int(k[0]), int(k[1]), int(k[2]), int(k[3]), 0, 0, 0, 0};
-  f32x4 s{0.f, 0.f, 0.f, 0.f};
-  s = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, q.hi, s, 4, 0, T, scale, 0, q.scale);
-  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, q.lo, s, 4, 0, T, scale, 1, q.scale);
 }
 
 template <bool HI>
@@ -273,7 +207,9 @@ __device__ __forceinline__ void chunk_scores(const Chunk<BITS>& c, const u32x4 (
 #pragma unroll
     for (int ks = 0; ks < 4; ++ks) {
       u32x4 kf;
-      if constexpr (BITS == 8) {
+      if constexpr (BITS == 4) {
+        kf = expand8(c.k[t][0][ks], __uint_as_float(c.ke[t] << 23));
+      } else if constexpr (BITS == 8) {
         const float sc = __uint_as_float(uint32_t(c.ke[t]) << 23);
         const uint32_t w0 = c.k[t][ks >> 1][2 * (ks & 1)], w1 = c.k[t][ks >> 1][2 * (ks & 1) + 1];
         kf = u32x4{expand2<false>(w0, sc), expand2<true>(w0, sc), expand2<false>(w1, sc), expand2<true>(w1, sc)};
@@ -413,14 +349,11 @@ __global__ __launch_bounds__(64 * W, 8 / W) void paged_attention(PagedArgs a, in
     const int row = min(rt * 16 + c16, rows - 1);   // past the end: the last row, never stored
     const int node = row / a.group;
     const int64_t from = (int64_t(q) * a.budget + node) * a.q_stride + (kvh * a.group + row - node * a.group) * kHead;
-    Parts4 qp;
-    // operand ks: dims 64 (ks / 2) + 16 g + 8 (ks % 2) .. + 7, for keys alike
-    auto load_query = [&] {
+    // operand ks: eight dims from here on, for keys alike (e2m1: a lane's dims are one block)
+    const int dim0 = BITS == 4 ? 32 * g : 16 * g;
+    auto dim_of = [&](int ks) { return BITS == 4 ? 8 * ks : 64 * (ks >> 1) + 8 * (ks & 1); };
 #pragma unroll
-      for (int ks = 0; ks < 4; ++ks)
-        qf[ks] = *reinterpret_cast<const u32x4*>(a.q + from + 64 * (ks >> 1) + 16 * g + 8 * (ks & 1));
-    };
-    if constexpr (BITS != 4) load_query();
+    for (int ks = 0; ks < 4; ++ks) qf[ks] = *reinterpret_cast<const u32x4*>(a.q + from + dim0 + dim_of(ks));
     const uint32_t* mrow = a.mask ? reinterpret_cast<const uint32_t*>(a.mask) + (int64_t(q) * a.budget + node) * words : nullptr;
     clear(st);
 
@@ -432,7 +365,6 @@ __global__ __launch_bounds__(64 * W, 8 / W) void paged_attention(PagedArgs a, in
     const int chunks = kb0 < ex.ctx ? min(min(step + n, nctx) - step, (ex.ctx - kb0 + kStep - 1) / kStep) : 0;
     if (chunks > 0) {
       Chunk<BITS> ch;
-      if constexpr (BITS == 4) qp = query_parts(a.q + from);
       f32x4 sc[2];
       u32x4 p;
       int p0, p1;   // pages of the halves of the chunk to fetch next
@@ -499,12 +431,7 @@ __global__ __launch_bounds__(64 * W, 8 / W) void paged_attention(PagedArgs a, in
           const int kb = kb0 + (i + 1) * kStep;
           const bool more = i + 1 < chunks;
           if (more) look_up(kb);
-          if constexpr (BITS == 4) {
-#pragma unroll
-            for (int t = 0; t < 2; ++t) sc[t] = scores4<0>(ch.k[t][0], int(ch.ke[t]), qp);
-          } else {
-            chunk_scores<BITS, TOP.value>(ch, qf, sc);
-          }
+          chunk_scores<BITS, TOP.value>(ch, qf, sc);
           uint32_t e0 = BITS == 8 ? ch.ke[0] : 0, e1 = BITS == 8 ? ch.ke[1] : 0;
           if (more) fetch_keys(kb);
           if constexpr (BITS == 8 && !TOP.value) {
@@ -541,7 +468,6 @@ __global__ __launch_bounds__(64 * W, 8 / W) void paged_attention(PagedArgs a, in
       return mrow ? mrow[kb >> 5] : node < kb ? 0u : node - kb >= 31 ? ~0u : (2u << (node - kb)) - 1u;
     };
     bool odd = false;   // the same for the wave
-    if constexpr (BITS == 4) load_query();
     for (int s = max(step, nctx); s < step + n; ++s) {
       const int kb = (s - nctx) * kStep + wave * kChunk;
       if (kb >= ex.nodes) break;
@@ -553,10 +479,10 @@ __global__ __launch_bounds__(64 * W, 8 / W) void paged_attention(PagedArgs a, in
       Chunk<16> ch;
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
-        const uint16_t* kp = a.k_tree + at(16 * t + c16) + 16 * g;
+        const uint16_t* kp = a.k_tree + at(16 * t + c16) + dim0;
 #pragma unroll
         for (int ks = 0; ks < 4; ++ks)
-          ch.k[t][ks] = *reinterpret_cast<const u32x4*>(kp + 64 * (ks >> 1) + 8 * (ks & 1));
+          ch.k[t][ks] = *reinterpret_cast<const u32x4*>(kp + dim_of(ks));
       }
 #pragma unroll
       for (int e = 0; e < 8; ++e)
@@ -659,7 +585,7 @@ __global__ __launch_bounds__(64 * W, 8 / W) void paged_attention(PagedArgs a, in
 
 // ---------------------------------------------------------------------------
 // Many rows: a block's W waves hold 16 RG query rows each and share tiles of 64
-// keys through LDS, in bf16 (e4m3 is converted once, as it is stored).  Tile
+// keys through LDS, in bf16 (e4m3 and e2m1 are converted once, as they are stored).  Tile
 // s + 1 travels in registers while tile s is multiplied, in two buffers.  A row
 // of 256 bytes keeps its 16-byte chunk c at c ^ k_place or c ^ v_place of the
 // row: K is read a row per lane, V transposed (ds_read_b64_tr_b16: lane l gets dim
@@ -669,9 +595,6 @@ __global__ __launch_bounds__(64 * W, 8 / W) void paged_attention(PagedArgs a, in
 // ---------------------------------------------------------------------------
 constexpr int kTile = 64;
 constexpr int kRowBytes = 2 * kHead, kTileBytes = kTile * kRowBytes;
-// A tile of keys in e2m1 and their exponents, values in bf16.
-constexpr int kKeys4 = kTile * (kHead / 2 + kHead / kBlock), kBuffer4 = kKeys4 + kTileBytes;
-static_assert(3 * kBuffer4 <= 4 * kTileBytes, "three buffers of e2m1 in the LDS of two of bf16");
 #define LDS_AS __attribute__((address_space(3)))
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef short s16x8 __attribute__((ext_vector_type(8)));
@@ -717,18 +640,6 @@ __global__ __launch_bounds__(64 * W, 8 / W) void paged_tiles(PagedArgs a, int wh
     const int kvh = item / ntile, rt = item - kvh * ntile;
 
     u32x4 qf[RG][4];
-    Parts4 qp[BITS == 4 ? RG : 1];
-    auto load_query = [&] {
-      const int tid = thread_again();
-#pragma unroll
-      for (int r = 0; r < RG; ++r) {
-        const int row = min(rt * kRows + (tid >> 6) * (16 * RG) + r * 16 + (tid & 15), rows - 1);   // past the end: the last row, never stored
-        const int node = row / a.group;
-        const uint16_t* from = a.q + (int64_t(q) * a.budget + node) * a.q_stride + (kvh * a.group + row - node * a.group) * kHead;
-#pragma unroll
-        for (int ks = 0; ks < 4; ++ks) qf[r][ks] = *reinterpret_cast<const u32x4*>(from + 32 * ks + 8 * ((tid & 63) >> 4));
-      }
-    };
     float m[RG], l[RG], bar[RG], ref[RG];   // bar: a score above it moves the reference m; ref = -m c2
     f32x4 o[RG][8];
     {
@@ -738,12 +649,8 @@ __global__ __launch_bounds__(64 * W, 8 / W) void paged_tiles(PagedArgs a, int wh
         const int row = min(rt * kRows + (tid >> 6) * (16 * RG) + r * 16 + (tid & 15), rows - 1);   // past the end: the last row, never stored
         const int node = row / a.group;
         const uint16_t* from = a.q + (int64_t(q) * a.budget + node) * a.q_stride + (kvh * a.group + row - node * a.group) * kHead;
-        if constexpr (BITS == 4) {
-          qp[r] = query_parts(from);
-        } else {
 #pragma unroll
-          for (int ks = 0; ks < 4; ++ks) qf[r][ks] = *reinterpret_cast<const u32x4*>(from + 32 * ks + 8 * ((tid & 63) >> 4));
-        }
+        for (int ks = 0; ks < 4; ++ks) qf[r][ks] = *reinterpret_cast<const u32x4*>(from + 32 * ks + 8 * ((tid & 63) >> 4));
         m[r] = bar[r] = -INFINITY;
         l[r] = ref[r] = 0.f;
 #pragma unroll
@@ -889,109 +796,6 @@ __global__ __launch_bounds__(64 * W, 8 / W) void paged_tiles(PagedArgs a, int wh
       }
     };
 
-    // The same of a context in e2m1, in three buffers, so that one barrier a tile will do,
-    // with the next tile stored first of all, the next products' operands read and the products
-    // spread between the exponentials (a wave waits for a product that finds the matrix cores
-    // busy), and the values' products ahead of the other wave of a SIMD, which has
-    // exponentials to do.  16 requests x 512 nodes over 2048 positions, 32 / 8 heads (us): in two
-    // buffers as above 399, in three 387, with the store first and the priority 353
-    // (344 in a graph, 1.0 PFLOP/s; e4m3 376); 2 x 16 nodes over 65536 70, 67, 64.  Of the
-    // 399, without the exponentials 49 less, without the values' reads and products 90,
-    // without the keys' 85.  Keys stay as they are held: a row of 64 bytes keeps its 16-byte
-    // piece c at c ^ (row / 4) % 4, behind the rows a word for each lane (r16, g): the
-    // exponents of keys r16, 16 + r16, ..
-    auto sweep4 = [&](const int first, const int end, auto&& fetch, auto&& store) __attribute__((always_inline)) {
-      if (first >= end) return;
-      const int k4 = r16 * (kHead / 2) + (g ^ (r16 >> 2)) * 16, e4 = kTile * (kHead / 2) + (4 * r16 + g) * 4;
-      struct Keys {
-        u32x4 k[2];
-        int e;
-      };
-      auto load_keys = [&](auto B, auto C, Keys& x) __attribute__((always_inline)) {
-        LDS_AS char* const kt = lds + B.value * kBuffer4;
-        x.e = *reinterpret_cast<const LDS_AS int*>(kt + e4);
-#pragma unroll
-        for (int t = 0; t < 2; ++t) x.k[t] = *reinterpret_cast<const LDS_AS u32x4*>(kt + k4 + (C.value * 32 + t * 16) * (kHead / 2));
-      };
-      auto load_values = [&](auto B, auto C, u32x4 (&vf)[8]) __attribute__((always_inline)) {
-#pragma unroll
-        for (int t = 0; t < 8; ++t) {
-          const LDS_AS char* at = lds + va[t] + (B.value * kBuffer4 + kKeys4 - kTileBytes + C.value * 32 * kRowBytes);
-          const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4*)at);
-          const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4*)(at + 16 * kRowBytes));
-          vf[t] = __builtin_bit_cast(u32x4, s16x8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]});
-        }
-      };
-      auto scores4_of = [&](auto C, const Keys& x, f32x4 (&sc)[RG][2]) __attribute__((always_inline)) {
-#pragma unroll
-        for (int r = 0; r < RG; ++r) {
-          sc[r][0] = scores4<2 * C.value>(x.k[0], x.e, qp[r]);
-          sc[r][1] = scores4<2 * C.value + 1>(x.k[1], x.e, qp[r]);
-        }
-      };
-      auto spread = [&] __attribute__((always_inline)) {
-        __builtin_amdgcn_sched_group_barrier(0x100, 19, 0);         // operands from LDS
-#pragma unroll
-        for (int i = 0; i < 4 * RG; ++i) {
-          __builtin_amdgcn_sched_group_barrier(0x402, 6, 0);        // weights
-          __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);        // scores
-        }
-      };
-      fetch(first);
-      uint64_t there = store(Index<0>());
-      if (first + 1 < end) fetch(first + 1);
-      __syncthreads();
-      f32x4 sa[RG][2], sb[RG][2];
-      u32x4 p[RG], vf[8];
-      Keys keys;
-      load_keys(Index<0>(), Index<0>(), keys);
-      scores4_of(Index<0>(), keys, sa);
-      auto values4 = [&] __attribute__((always_inline)) {
-        __builtin_amdgcn_s_setprio(1);
-#pragma unroll
-        for (int t = 0; t < 8; ++t)
-#pragma unroll
-          for (int r = 0; r < RG; ++r) o[r][t] = mfma16(vf[t], p[r], o[r][t]);
-        __builtin_amdgcn_s_setprio(0);
-      };
-      auto tile = [&](auto B, int s) __attribute__((always_inline)) {
-        const Index<(B.value + 1) % 3> next;
-        const bool masked = there != ~0ull;
-        uint32_t seen[2][RG];
-#pragma unroll
-        for (int r = 0; r < RG; ++r) {
-          seen[0][r] = uint32_t(there);
-          seen[1][r] = uint32_t(there >> 32);
-        }
-        if (s + 1 < end) {
-          there = store(next);
-          if (s + 2 < end) fetch(s + 2);
-        }
-        settle(masked, seen[0], sa);
-        load_values(B, Index<0>(), vf);
-        load_keys(B, Index<1>(), keys);
-        scores4_of(Index<1>(), keys, sb);
-        weights(sa, p);
-        values4();
-        spread();
-        settle(masked, seen[1], sb);
-        __syncthreads();
-        load_values(B, Index<1>(), vf);
-        load_keys(next, Index<0>(), keys);
-        scores4_of(Index<0>(), keys, sa);   // after the last tile: not used
-        weights(sb, p);
-        values4();
-        spread();
-      };
-#pragma unroll 1
-      for (int s = first; s < end; s += 3) {
-        tile(Index<0>(), s);
-        if (s + 1 < end) tile(Index<1>(), s + 1);
-        if (s + 2 < end) tile(Index<2>(), s + 2);
-      }
-      __syncthreads();   // the buffers are free again
-    };
-
     {   // the context
       const int32_t* table = a.c.table + int64_t(q) * a.c.max_pages;
       constexpr int kRowsWave = BITS == 16 ? 4 : 8, kShares = kTile / (kRowsWave * W);
@@ -1033,22 +837,20 @@ __global__ __launch_bounds__(64 * W, 8 / W) void paged_tiles(PagedArgs a, int wh
       auto store = [&](auto B) __attribute__((always_inline)) -> uint64_t {
         const uint64_t there = in_flight;
         const Piece zero = {};
-        LDS_AS char* const kt = lds + B.value * (BITS == 4 ? kBuffer4 : 2 * kTileBytes);
+        LDS_AS char* const kt = lds + B.value * 2 * kTileBytes;
 #pragma unroll
         for (int i = 0; i < kShares; ++i) {
           const int key = first_key(i) + (BITS == 16 ? g : lane >> 3);
           const bool gone = there != ~0ull && !((there >> key) & 1);
           if (gone) vx[i] = zero;
           if constexpr (BITS == 4) {
-            const float sv = gone ? 1.f : __uint_as_float(ve[i] << 23);
+            const float sk = __uint_as_float(ke[i] << 23), sv = gone ? 1.f : __uint_as_float(ve[i] << 23);
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
               const int c = 2 * (lane & 7) + h;
-              *reinterpret_cast<LDS_AS u32x4*>(kt + kKeys4 + key * kRowBytes + (c ^ v_place(key)) * 16) = expand8(vx[i][h], sv);
+              *reinterpret_cast<LDS_AS u32x4*>(kt + key * kRowBytes + (c ^ k_place(key)) * 16) = expand8(kx[i][h], sk);
+              *reinterpret_cast<LDS_AS u32x4*>(kt + kTileBytes + key * kRowBytes + (c ^ v_place(key)) * 16) = expand8(vx[i][h], sv);
             }
-            const int c = (lane & 7) >> 1;   // keys stay as they are
-            *reinterpret_cast<LDS_AS u32x2*>(kt + key * (kHead / 2) + (c ^ ((key >> 2) & 3)) * 16 + (lane & 1) * 8) = kx[i];
-            *reinterpret_cast<LDS_AS uint8_t*>(kt + kTile * (kHead / 2) + (4 * (key & 15) + c) * 4 + (key >> 4)) = uint8_t(ke[i]);
           } else if constexpr (BITS == 8) {
             const float sk = __uint_as_float(ke[i] << 23), sv = gone ? 1.f : __uint_as_float(ve[i] << 23);
             u32x4 k[2], v[2];
@@ -1080,10 +882,8 @@ __global__ __launch_bounds__(64 * W, 8 / W) void paged_tiles(PagedArgs a, int wh
         return there;
       };
       if (step < min(last, nctx)) look_up(step);
-      if constexpr (BITS == 4) sweep4(step, min(last, nctx), fetch, store);
-      else sweep(step, min(last, nctx), fetch, store, [&](int, int, uint64_t there) { return there; }, false);
+      sweep(step, min(last, nctx), fetch, store, [&](int, int, uint64_t there) { return there; }, false);
     }
-    if constexpr (BITS == 4) load_query();
     const int tid = thread_again();
     int node[RG], row[RG];
 #pragma unroll

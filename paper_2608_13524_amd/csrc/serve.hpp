@@ -22,14 +22,6 @@ __device__ __forceinline__ uint32_t finite_pair(uint32_t w) {   // two bf16
   return w;
 }
 
-// Least e >= LOW with amax <= 448 * 2^e = 1.75 * 2^(e + 8).
-template <int LOW = kExpLow>
-__device__ __forceinline__ int row_exponent(float amax) {
-  const uint32_t u = __float_as_uint(amax);
-  const int e = int(u >> 23) - 127 - 8 + ((u & 0x7FFFFFu) > 0x600000u);
-  return min(max(e, LOW), 120);
-}
-
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 // Eight e2m1 elements times a power of two in bf16, exact.  The conversion takes the
