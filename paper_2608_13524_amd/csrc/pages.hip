@@ -32,7 +32,7 @@ struct Space {
   int32_t* upto;
   int32_t* list;
 };
-__host__ __device__ inline int words_of(int num_pages) { return (num_pages + 31) / 32; }
+__host__ __device__ inline int words_of(int num_pages) { return int((int64_t(num_pages) + 31) / 32); }
 __host__ __device__ inline int64_t padded(int64_t n) { return (n + 63) & ~int64_t(63); }
 __device__ __forceinline__ Space space_of(const PagesArgs& a) {
   const int64_t words = padded(words_of(a.num_pages));
