@@ -78,7 +78,9 @@ typedef struct dartree_rotary_params {
  * q: row i of request r at (r * rows + i) * q_stride elements, heads_q * head_dim
  * elements each; k, q_out and k_out likewise with strides of their own, multiples of
  * 8.  q_out may be q with the same stride (elements past rotary_dim are not touched
- * then), k_out likewise k; otherwise outputs overlap nothing that the call reads.
+ * then), k_out likewise k; otherwise an output's rows overlap neither q's nor k's rows
+ * nor the other output's, which is checked (rows side by side in one tensor do not
+ * overlap), nor anything else that the call reads.
  * Angles in 64-bit integers, sines and cosines to 2^-23, products in fp32; bf16
  * outputs are rounded once.  batch * rows <= 2^24. */
 dartree_status dartree_rotary(const dartree_rotary_params* p, const uint64_t* turns, const void* q, int64_t q_stride,

@@ -140,6 +140,41 @@ bool rotary_rows_ok(const dartree_rotary_params& p, int heads, const void* x, in
   return given(x) && given(out) && stride_ok(stride, row) && stride_ok(out_stride, row) && (x != out || stride == out_stride);
 }
 
+// `count` rows of `bytes`, `step` bytes apart.
+struct RowSet {
+  uintptr_t at;
+  int64_t bytes, step, count;
+};
+// No byte in common: the sets follow each other, or each lies beside the other's rows, as parts of the
+// rows of one tensor do (exact for one step; for two, of all rows that lie so).
+bool rows_apart(const RowSet& x, const RowSet& y) {
+  const auto end = [](const RowSet& r) { return __int128(r.at) + __int128(r.count - 1) * r.step + r.bytes; };
+  if (end(x) <= __int128(y.at) || end(y) <= __int128(x.at)) return true;
+  if (x.count == 1) return false;
+  int64_t gap = x.step, r = y.step;   // their greatest common divisor
+  while (r != 0) {
+    const int64_t t = gap % r;
+    gap = r;
+    r = t;
+  }
+  const int64_t d = int64_t((__int128(y.at) - __int128(x.at)) % gap), beside = d < 0 ? d + gap : d;
+  return beside >= x.bytes && beside + y.bytes <= gap;
+}
+
+// The outputs are their inputs, or apart from both inputs, and from each other.
+bool rotary_apart(const dartree_rotary_params& p, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                  const void* q_out, int64_t q_out_stride, const void* k_out, int64_t k_out_stride) {
+  const int64_t size = p.type == DARTREE_BF16 ? 2 : 4, count = int64_t(p.batch) * p.rows;
+  const auto rows = [&](const void* at, int heads, int64_t stride) {
+    return RowSet{reinterpret_cast<uintptr_t>(at), heads * int64_t(p.head_dim) * size, stride * size, count};
+  };
+  const RowSet qi = rows(q, p.heads_q, q_stride), qo = rows(q_out, p.heads_q, q_out_stride);
+  const RowSet ki = rows(k, p.heads_kv, k_stride), ko = rows(k_out, p.heads_kv, k_out_stride);
+  if (p.heads_q > 0 && q != q_out && !rows_apart(qi, qo)) return false;
+  if (p.heads_kv > 0 && k != k_out && !rows_apart(ki, ko)) return false;
+  return p.heads_q == 0 || p.heads_kv == 0 || (rows_apart(qo, ki) && rows_apart(qo, ko) && rows_apart(qi, ko));
+}
+
 // The fraction of a turn in `radians`, in units of 2^-64 (x87's 64 bits of mantissa).
 uint64_t turn_of(long double radians) {
   const long double pi = 3.14159265358979323846264338327950288L;
@@ -452,6 +487,7 @@ dartree_status dartree_rotary(const dartree_rotary_params* p, const uint64_t* tu
   if (!rotary_rows_ok(*p, p->heads_q, q, q_stride, q_out, q_out_stride) ||
       !rotary_rows_ok(*p, p->heads_kv, k, k_stride, k_out, k_out_stride))
     return DARTREE_ERR_INVALID_ARG;
+  if (!rotary_apart(*p, q, q_stride, k, k_stride, q_out, q_out_stride, k_out, k_out_stride)) return DARTREE_ERR_INVALID_ARG;
   RotaryArgs a{};
   a.batch = p->batch;
   a.rows = p->rows;
