@@ -82,7 +82,7 @@ typedef struct dartree_rotary_params {
  * nor the other output's, which is checked (rows side by side in one tensor do not
  * overlap), nor anything else that the call reads.
  * Angles in 64-bit integers, sines and cosines to 2^-23, products in fp32; bf16
- * outputs are rounded once.  batch * rows <= 2^24. */
+ * outputs are rounded once.  batch * rows < 2^24. */
 dartree_status dartree_rotary(const dartree_rotary_params* p, const uint64_t* turns, const void* q, int64_t q_stride,
                               const void* k, int64_t k_stride, void* q_out, int64_t q_out_stride, void* k_out,
                               int64_t k_out_stride, const int32_t* positions, const int32_t* start,
