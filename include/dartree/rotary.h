@@ -47,13 +47,18 @@ typedef struct dartree_rotary_scaling {
 /* The table of frequencies that dartree_rotary reads, for rotary_dim / 2 pairs
  * (host only, `turns` is host memory): turns[i] is the fraction of a turn that
  * pair i makes from one position to the next, in units of 2^-64.  A position's
- * angle is their product modulo one turn, exact in 64-bit integers: at position
- * 2^20 it is good to 2^-43 of a turn.  scaling NULL: PLAIN.  rotary_dim: even,
- * 2 .. 512; base > 0, finite. */
+ * angle is their product modulo one turn, exact in 64-bit integers.  A pair of f
+ * radians a position is within two units where f <= 1, so that its angle at position
+ * 2^20 is good to 2^-43 of a turn, and within about 2 f units where it is faster
+ * (frequencies are formed in 64 bits of mantissa).  scaling NULL: PLAIN.
+ * rotary_dim: even, 2 .. 512; base > 0, finite. */
 dartree_status dartree_rotary_turns(int32_t rotary_dim, double base, const dartree_rotary_scaling* scaling,
                                     uint64_t* turns);
 
-/* The same table of any `pairs` finite frequencies, in radians a position (host only). */
+/* The same table of any `pairs` finite frequencies, in radians a position (host only),
+ * within one unit each (up to 2^60 radians).  For rules that are not among those above,
+ * such as a ramp over the pairs' numbers i between two bounds in the place of TURNS'
+ * over their turns n_i, which gives other angles: a model's own rule decides. */
 dartree_status dartree_rotary_turns_of(int32_t pairs, const double* radians, uint64_t* turns);
 
 typedef struct dartree_rotary_params {

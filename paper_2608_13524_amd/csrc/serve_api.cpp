@@ -175,12 +175,14 @@ bool rotary_apart(const dartree_rotary_params& p, const void* q, int64_t q_strid
   return p.heads_q == 0 || p.heads_kv == 0 || (rows_apart(qo, ki) && rows_apart(qo, ko) && rows_apart(qi, ko));
 }
 
-// The fraction of a turn in `radians`, in units of 2^-64 (x87's 64 bits of mantissa).
+// The fraction of a turn in `radians`, in units of 2^-64.  1 / (2 pi) in two numbers of 64 bits of
+// mantissa (x87), so that the whole turns of fast pairs take no bits from it: within a unit up to 2^60.
 uint64_t turn_of(long double radians) {
-  const long double pi = 3.14159265358979323846264338327950288L;
-  long double t = fmodl(radians / (2 * pi), 1.0L);
+  const long double high = 0.159154943091895335769L, low = -2.03622285290738401775e-22L;
+  const long double p = radians * high, rest = fmal(radians, high, -p) + radians * low;
+  long double t = fmodl(fmodl(p, 1.0L) + rest, 1.0L);
   if (t < 0) t += 1.0L;
-  const long double u = floorl(t * 18446744073709551616.0L + 0.5L);
+  const long double u = rintl(t * 18446744073709551616.0L);
   return u >= 18446744073709551616.0L ? 0 : uint64_t(u);
 }
 
