@@ -18,12 +18,12 @@
 // of its query.  A tile lies in one page, so every load has a scalar base and an
 // offset that is the lane's own.  Keys in e4m3 become bf16 on the way with their
 // power of two applied by the conversion (exact), and so do those in e2m1, eight from a
-// word.
-// 64 single tokens over up to 8192 positions, 32 / 8 heads, e2m1: 428 MB in 91 us, 4.7
-// TB/s, as a large copy runs; without the conversions 88, with two chunks ahead or
-// pages looked up earlier 91 to 93.  A head's keys and values are read
-// once for 16 query rows (again for the next 16, from a cache where it holds them)
-// and never pass through LDS.
+// word.  (The scaled matrix instruction would take e2m1 keys as they are, but aligns
+// eight products at a time to the largest and keeps 13 bits below it, measured; bf16's
+// keep 24.  It was 8 to 12 % faster for many rows, no faster here.)  64 single tokens
+// over up to 8192 positions, 32 / 8 heads, e2m1: 428 MB in 93 us, 4.6 TB/s, as a large
+// copy runs.  A head's keys and values are read once for 16 query rows (again for the
+// next 16, from a cache where it holds them) and never pass through LDS.
 //
 // More rows (paged_tiles): below.
 #include <algorithm>
@@ -1163,7 +1163,7 @@ Plan plan_of(int batch, int budget, int max_ctx, int heads_q, int heads_kv, int 
   // 375, 17 468 / 480, 32 ragged 741 / 707; 4 over 500 positions 69 / 53, over 16000
   // 632 / 575; bf16 alike.  e2m1 chooses alike: 1 request x 64 nodes over 2048 positions
   // whole 15.9, shared 19.9, tiles of 64 rows 26, of 128 36; 2 x 16 nodes over 65536
-  // tiles of 64 rows 72 (64 now), 16 rows shared 91, tiles of 128 98.
+  // tiles of 64 rows 70 to 72, 16 rows shared 91, tiles of 128 98.  (16 x 512 over 2048: 395.)
   const bool wide = tiles_of(256) >= 192 && 10 * 256 * tiles_of(256) <= 11 * 128 * tiles_of(128);
   p.kernel = rows <= 16 || middle ? kFew : rows <= 64 || tiles_of(128) * steps < 8 * kResident ? kTiles64 : wide ? kTiles256 : kTiles128;
   p.rows = p.kernel == kFew ? 16 : p.kernel == kTiles64 ? 64 : p.kernel == kTiles128 ? 128 : 256;

@@ -8,7 +8,7 @@
 //
 // What bounds them is latency: a launch (2.2 us each), the round trips start -> table
 // entry -> bitmap -> page, and a barrier or two a prefix sum.  64 requests of 4096
-// positions in pages of 64: fork 2.4 us, reserve 8.1 (as three launches 14.4).  A compact
+// positions in pages of 64: fork 2.3 us, reserve 8.4 (as three launches 14.4).  A compact
 // of a table of 8320 entries and as many pages 11 (as four launches 18).
 #include <algorithm>
 
@@ -301,7 +301,8 @@ hipError_t launch_scan(const PagesArgs& a, hipStream_t s) {
 
 // A unit of the copy: 16 KB of a page's keys or values, or a page's exponents; a
 // thread has four loads of 16 bytes in flight.  Bound by memory: 512 MB read and
-// written (compact) in 92 us, 5.6 TB/s; 134 MB in 13.5, as far as the caches hold them.
+// written (compact, e4m3) in 92 us, 5.6 TB/s; 975 MB of e2m1 pages in 188, 5.2; 134 MB in
+// 13.8, 71 in e2m1 in 11.8, as far as the caches hold them.
 constexpr int kUnit = 16384;
 __global__ __launch_bounds__(kThreads) void cache_copy(PageCopyArgs a) {
   const int pairs = min(a.count[0], a.max_pairs);

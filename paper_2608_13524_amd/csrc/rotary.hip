@@ -12,7 +12,10 @@
 // Bound by HBM from about a thousand rows on (8 x 2048 rows of 32 + 8 heads in bf16: 252 MB of
 // a ragged batch in 45 us, 5.6 TB/s), by the launch below that (64 rows 3.9 us).  An item
 // is read, turned and written before the next: four of a thread in flight took 61 us
-// there, 86 for 62 with interleaved pairs.
+// there, 86 for 62 with interleaved pairs.  Lengths off the vector width (V 1) go
+// element by element, the copied part too: 16384 rows of 40 heads of 128, halves, in bf16 61
+// us (5.5 TB/s) whole, 159 for 126 turned, 200 for 36 and 24, 213 for 2; in fp32 117, 190,
+// 245 (24: 127, vectors) and 265.
 #include "internal.hpp"
 #include "rotary.hpp"
 
